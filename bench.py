@@ -40,7 +40,7 @@ KERNEL_NAMES = {"gate_up": "gemm_kernel<bf16,MG=1,EPI_SWIGLU> (gate/up projectio
 TRAFFIC_PROFILES = {"gate_up": "profiles/gemm_gate_up_7b_b1_k4_traffic.md"}
 # the device code of every kernel and the launch rules: a counter summary stands only while these are unchanged
 KERNEL_SOURCES = tuple("paper_2510_05421_amd/csrc/" + f
-                       for f in ("kernels.hip", "prefill.hip", "device.h", "kernels.h", "ring.h"))
+                       for f in ("kernels.hip", "prefill.hip", "learn.hip", "device.h", "kernels.h", "learn.h", "ring.h"))
 
 
 def kernel_sources_sha256():

@@ -249,6 +249,127 @@ typedef struct {
 
 dvi_status dvi_update_drafter(dvi_ctx *ctx, const dvi_update_args *args, dvi_update_stats *stats);
 
+/* ---- learning operators on the caller's tensors --------------------------------------------
+ *
+ * What a drafter's training (Section 3.4) does apart from the replay ring, for rows and parameters
+ * that the caller holds: log-probabilities of tokens, a clipped policy loss with its gradient, and
+ * AdamW over many tensors.  No context: every call names its stream, whose device must be current and
+ * hold all DEVICE arguments, and a workspace (DEVICE, 256-byte aligned, at least the bytes of the
+ * call's own _workspace_bytes; its contents need not be kept).  Nothing is allocated, copied to the
+ * host or waited for, so every call can be captured into a HIP graph (which replays it with the host
+ * values it was captured with, an AdamW step's number among them).  Two calls in flight at the same time need two workspaces.  Repeated
+ * calls on the same inputs give the same bits.  Errors: DVI_ERR_ARG, DVI_ERR_CAPACITY (workspace too
+ * small) before anything is launched, DVI_ERR_DEVICE from a launch; dvi_op_error describes the
+ * calling thread's last one.
+ */
+const char *dvi_op_error(void);
+
+/*
+ * Rows of logits: DEVICE [rows, vocab] of dtype, row i at logits + i * ld elements (ld >= 0, any
+ * alignment of its elements; rows may overlap, as an expanded row's do; at most 2^22 rows); temperature
+ * > 0 divides them.
+ * tokens: DEVICE int32 [rows].  A row whose token lies outside [0, vocab) or that has no logit above
+ * -inf is masked: its outputs are 0.  Logits of -inf (or the type's lowest number) are tokens of
+ * probability 0.  A NaN, or +inf, among a row's logits makes its outputs NaN.
+ *
+ * dvi_token_logprobs: logp[i] = log softmax(logits_i / temperature)[tokens_i] and, unless NULL,
+ * entropy[i] = -sum p log p.  DEVICE fp32 [rows].
+ */
+typedef struct {
+    int64_t rows;
+    int32_t vocab;
+    dvi_dtype dtype;
+    const void *logits;
+    int64_t ld;
+    const int32_t *tokens;
+    double temperature;
+    float *logp;
+    float *entropy;
+} dvi_logprob_args;
+size_t dvi_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab);
+dvi_status dvi_token_logprobs(const dvi_logprob_args *args, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Clipped policy loss over rows of logits (as above), with its gradient:
+ *   lp = log p(token), ratio = exp(lp - old_logp), A = advantages
+ *   policy = -min(ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A)
+ *   kl     = KL(p || softmax(ref_logits / ref_temperature)), or with ref_logp = log q(token) the
+ *            estimate exp(ref_logp - lp) - (ref_logp - lp) - 1, or 0 with neither
+ *   loss   = sum_i weights_i (policy_i + c_kl kl_i - c_ent entropy_i)
+ * Rows of weight 0 are masked too: nothing else of them is read.  The caller's weights carry the
+ * mean over tokens or sequences (weights NULL: 1 / rows each).  old_logp NULL: every ratio is 1, the
+ * plain policy gradient.  advantages, old_logp, weights, ref_logp: DEVICE fp32 [rows].  ref_logits:
+ * DEVICE, dtype and shape of logits, row stride ref_ld; at most one of ref_logits and ref_logp; a row
+ * of ref_logits without any logit above -inf masks the row, and one that gives probability 0 to a
+ * token that p has makes kl infinite.
+ * grad: NULL, or DEVICE [rows, vocab] of dtype (row stride grad_ld >= vocab) receiving d loss / d logits,
+ * 0 in masked rows; it may be the logits themselves (same ld), and overlaps no other argument.
+ * logp: NULL or DEVICE fp32 [rows].  terms: DEVICE fp32 [5], the weighted sums loss, policy, kl,
+ * entropy, and the weight of the clipped rows.
+ */
+typedef struct {
+    int64_t rows;
+    int32_t vocab;
+    dvi_dtype dtype;
+    const void *logits;
+    int64_t ld;
+    const int32_t *tokens;
+    const float *advantages;
+    const float *old_logp;
+    const float *weights;
+    const void *ref_logits;
+    int64_t ref_ld;
+    const float *ref_logp;
+    double temperature, ref_temperature;
+    double clip_low, clip_high;   /* 0 <= clip_low <= 1, 0 <= clip_high */
+    double c_kl, c_ent;
+    void *grad;
+    int64_t grad_ld;
+    float *logp;
+    float *terms;
+} dvi_policy_args;
+size_t dvi_policy_loss_workspace_bytes(int64_t rows, int32_t vocab);
+dvi_status dvi_policy_loss(const dvi_policy_args *args, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/*
+ * One AdamW step over n_tensors parameter tensors (HOST array of descriptors of contiguous DEVICE arrays
+ * of n elements each; n may be 0, and all together at most 2^35), decoupled weight decay, step number step >= 1:
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2
+ *   p <- p - lr weight_decay p - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
+ * max_norm > 0: the norm of all gradients together goes to grad_norm (NULL or DEVICE fp32 [1]); a norm
+ * above max_norm scales the gradients down to it, and one that is not finite leaves every tensor and
+ * state as it is.  max_norm = +inf only measures and guards; with 0 nothing is measured, and
+ * grad_norm must be NULL.
+ * Parameters of dtype, gradients of grad_dtype.  master: NULL, or the fp32 values that a bf16 parameter
+ * is the rounding of (then all tensors have one).
+ * state_bits 32: m and v are fp32.  state_bits 8: m and v hold OCP e4m3 codes of m and of sqrt(v), times
+ * a scale per block of 256 elements of a tensor (m_scale, v_scale: fp32 [(n + 255) / 256], the block's
+ * largest magnitude / 448), rounded up or down at random with the exact mean; the random bits are a
+ * function of seed, step and the element's number, tensors counted in whole blocks one after the other.
+ * All-zero bytes are the initial state of either kind.  Arrays overlap no other array of the call.
+ */
+typedef struct {
+    int64_t n;
+    void *param;
+    float *master;
+    const void *grad;
+    void *m;
+    void *v;
+    float *m_scale;
+    float *v_scale;
+} dvi_adamw_tensor;
+typedef struct {
+    dvi_dtype dtype, grad_dtype;
+    int32_t state_bits;
+    int32_t step;
+    double lr, beta1, beta2, eps, weight_decay, max_norm;
+    uint64_t seed;
+    float *grad_norm;
+} dvi_adamw_args;
+size_t dvi_adamw_workspace_bytes(int32_t n_tensors);
+dvi_status dvi_adamw(const dvi_adamw_tensor *tensors, int32_t n_tensors, const dvi_adamw_args *args, void *workspace,
+                     size_t ws_bytes, void *hip_stream);
+
 /* Message for the last error on this context (static storage; never NULL). */
 const char *dvi_last_error(const dvi_ctx *ctx);
 

@@ -12,4 +12,7 @@ def __getattr__(name):
     if name in ("Engine", "EngineConfig", "workspace_bytes"):
         from . import engine
         return getattr(engine, name)
+    if name in ("AdamW", "PolicyLoss", "policy_loss", "token_logprobs"):
+        from . import learn
+        return getattr(learn, name)
     raise AttributeError(name)

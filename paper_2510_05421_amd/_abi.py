@@ -12,6 +12,7 @@ FP32, BF16 = 0, 1
 PROBES = {"off": 0, "qkv": 1, "attn_out": 2, "gate_up": 3, "down": 4, "head": 5, "attention": 6}
 
 c_i32, c_f32, c_vp = ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
+c_i64, c_f64, c_size = ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
 P_i32 = ctypes.POINTER(ctypes.c_int32)
 
 
@@ -42,6 +43,30 @@ class UpdateStats(ctypes.Structure):
                 ("rows", c_i32), ("accepted", c_i32), ("fresh", c_i32), ("fresh_accepted", c_i32)]
 
 
+class LogprobArgs(ctypes.Structure):
+    _fields_ = [("rows", c_i64), ("vocab", c_i32), ("dtype", c_i32), ("logits", c_vp), ("ld", c_i64), ("tokens", c_vp),
+                ("temperature", c_f64), ("logp", c_vp), ("entropy", c_vp)]
+
+
+class PolicyArgs(ctypes.Structure):
+    _fields_ = [("rows", c_i64), ("vocab", c_i32), ("dtype", c_i32), ("logits", c_vp), ("ld", c_i64), ("tokens", c_vp),
+                ("advantages", c_vp), ("old_logp", c_vp), ("weights", c_vp), ("ref_logits", c_vp), ("ref_ld", c_i64),
+                ("ref_logp", c_vp), ("temperature", c_f64), ("ref_temperature", c_f64), ("clip_low", c_f64),
+                ("clip_high", c_f64), ("c_kl", c_f64), ("c_ent", c_f64), ("grad", c_vp), ("grad_ld", c_i64),
+                ("logp", c_vp), ("terms", c_vp)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("n", c_i64), ("param", c_vp), ("master", c_vp), ("grad", c_vp), ("m", c_vp), ("v", c_vp),
+                ("m_scale", c_vp), ("v_scale", c_vp)]
+
+
+class AdamwArgs(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("grad_dtype", c_i32), ("state_bits", c_i32), ("step", c_i32), ("lr", c_f64),
+                ("beta1", c_f64), ("beta2", c_f64), ("eps", c_f64), ("weight_decay", c_f64), ("max_norm", c_f64),
+                ("seed", ctypes.c_uint64), ("grad_norm", c_vp)]
+
+
 # name -> (restype, argtypes)
 SIGNATURES = {
     "dvi_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Config)]),
@@ -56,6 +81,13 @@ SIGNATURES = {
     "dvi_decode_steps": (c_i32, [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp]),
     "dvi_abort_step": (c_i32, [c_vp]),
     "dvi_update_drafter": (c_i32, [c_vp, ctypes.POINTER(UpdateArgs), ctypes.POINTER(UpdateStats)]),
+    "dvi_op_error": (ctypes.c_char_p, []),
+    "dvi_token_logprobs_workspace_bytes": (c_size, [c_i64, c_i32]),
+    "dvi_token_logprobs": (c_i32, [ctypes.POINTER(LogprobArgs), c_vp, c_size, c_vp]),
+    "dvi_policy_loss_workspace_bytes": (c_size, [c_i64, c_i32]),
+    "dvi_policy_loss": (c_i32, [ctypes.POINTER(PolicyArgs), c_vp, c_size, c_vp]),
+    "dvi_adamw_workspace_bytes": (c_size, [c_i32]),
+    "dvi_adamw": (c_i32, [ctypes.POINTER(AdamwTensor), c_i32, ctypes.POINTER(AdamwArgs), c_vp, c_size, c_vp]),
     "dvi_last_error": (ctypes.c_char_p, [c_vp]),
     "dvi_read_kv": (c_i32, [c_vp, c_i32, c_i32, c_i32, c_i32, c_vp, c_vp]),
     "dvi_read_logits": (c_i32, [c_vp, c_vp]),

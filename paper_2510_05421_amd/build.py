@@ -7,7 +7,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libdvi.so")
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("kernels.hip", "prefill.hip", "engine.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("kernels.hip", "prefill.hip", "learn.hip", "engine.hip")]
 ARCH = os.environ.get("DVI_OFFLOAD_ARCH", "gfx950")
 
 HIPCC_FLAGS = [

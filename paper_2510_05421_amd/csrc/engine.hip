@@ -17,6 +17,7 @@
 
 #include "../../include/dvi.h"
 #include "kernels.h"
+#include "learn.h"
 
 using namespace dvi;
 
@@ -1324,6 +1325,266 @@ extern "C" dvi_status dvi_update_drafter(dvi_ctx *x, const dvi_update_args *ua, 
         stats->fresh_accepted = (int32_t)lo[8];
     }
     return DVI_OK;
+}
+
+// ------------------------------------------------------------------------------------------
+// C ABI: learning operators on the caller's tensors
+// ------------------------------------------------------------------------------------------
+static thread_local char op_err[256];
+
+static dvi_status op_fail(dvi_status s, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(op_err, sizeof(op_err), fmt, ap);
+    va_end(ap);
+    return s;
+}
+
+extern "C" const char *dvi_op_error(void) { return op_err; }
+
+static DType op_dtype(dvi_dtype t) { return t == DVI_BF16 ? DType::BF16 : DType::F32; }
+static size_t op_size(dvi_dtype t) { return t == DVI_BF16 ? 2 : 4; }
+
+static dvi_status op_workspace(const void *ws, size_t have, size_t need) {
+    if (have < need) return op_fail(DVI_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", have, need);
+    if (need && (ws == nullptr || (uintptr_t)ws % 256)) return op_fail(DVI_ERR_ARG, "workspace must be 256-byte aligned");
+    return DVI_OK;
+}
+
+static dvi_status op_launched(void) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? DVI_OK : op_fail(DVI_ERR_DEVICE, "kernel launch: %s", hipGetErrorString(e));
+}
+
+// Rows of logits at an address: where they begin and end, in bytes.
+struct Extent {
+    uintptr_t lo, hi;
+};
+static Extent rows_extent(const void *p, int64_t rows, int64_t ld, int32_t vocab, size_t es) {
+    const uintptr_t b = (uintptr_t)p;
+    return {b, b + (size_t)((rows - 1) * ld + vocab) * es};
+}
+static bool apart(Extent a, Extent b) { return a.hi <= b.lo || b.hi <= a.lo; }
+
+// Whether two sets of rows share no element: extents that do not meet, or rows of one stride interleaved.
+static bool rows_apart(const void *p, int64_t pld, const void *q, int64_t qld, int64_t rows, int32_t vocab, size_t es) {
+    if (apart(rows_extent(p, rows, pld, vocab, es), rows_extent(q, rows, qld, vocab, es))) return true;
+    if (pld != qld || rows < 2) return false;
+    const int64_t row = pld * (int64_t)es, width = vocab * (int64_t)es;
+    const int64_t off = (((int64_t)((uintptr_t)q - (uintptr_t)p)) % row + row) % row;
+    return off >= width && off <= row - width;
+}
+
+// The largest number of rows (a launch's threads are counted in 32 bits), and the widest stride.
+static constexpr int64_t kMaxOpRows = (int64_t)1 << 22, kMaxOpStride = (int64_t)1 << 36;
+
+static dvi_status check_rows(int64_t rows, int32_t vocab, dvi_dtype dtype, const void *logits, int64_t ld,
+                             const int32_t *tokens, double temperature) {
+    if (dtype != DVI_FP32 && dtype != DVI_BF16) return op_fail(DVI_ERR_ARG, "dtype must be DVI_FP32 or DVI_BF16");
+    if (rows < 0) return op_fail(DVI_ERR_ARG, "rows must not be negative");
+    if (rows > kMaxOpRows) return op_fail(DVI_ERR_CAPACITY, "at most %lld rows", (long long)kMaxOpRows);
+    if (vocab < 1) return op_fail(DVI_ERR_ARG, "vocab must be at least 1");
+    if (!(temperature > 0.0) || !(temperature < 1e30)) return op_fail(DVI_ERR_ARG, "temperature must be > 0 and finite");
+    if (rows == 0) return DVI_OK;
+    if (logits == nullptr || tokens == nullptr) return op_fail(DVI_ERR_ARG, "logits and tokens must be given");
+    if (ld < 0 || ld > kMaxOpStride) return op_fail(DVI_ERR_ARG, "row strides from 0 to 2^36");
+    if ((uintptr_t)logits % op_size(dtype)) return op_fail(DVI_ERR_ARG, "logits are not aligned to their type");
+    return DVI_OK;
+}
+
+extern "C" size_t dvi_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab) {
+    return rows < 0 || rows > kMaxOpRows || vocab < 1 ? 0 : rows_workspace(rows, vocab, false);
+}
+
+extern "C" dvi_status dvi_token_logprobs(const dvi_logprob_args *g, void *workspace, size_t ws_bytes, void *hip_stream) {
+    if (!g) return op_fail(DVI_ERR_ARG, "null arguments");
+    dvi_status st = check_rows(g->rows, g->vocab, g->dtype, g->logits, g->ld, g->tokens, g->temperature);
+    if (st != DVI_OK) return st;
+    if (g->rows == 0) return DVI_OK;
+    if (!g->logp) return op_fail(DVI_ERR_ARG, "logp must be given");
+    st = op_workspace(workspace, ws_bytes, rows_workspace(g->rows, g->vocab, false));
+    if (st != DVI_OK) return st;
+    RowArgs a{};
+    a.z = g->logits;
+    a.ldz = g->ld;
+    a.tok = g->tokens;
+    a.N = g->rows;
+    a.V = g->vocab;
+    a.it = a.iq = 1.0 / g->temperature;
+    a.logp = g->logp;
+    a.entropy = g->entropy;
+    launch_rows(op_dtype(g->dtype), a, workspace, (hipStream_t)hip_stream);
+    return op_launched();
+}
+
+extern "C" size_t dvi_policy_loss_workspace_bytes(int64_t rows, int32_t vocab) {
+    return rows < 0 || rows > kMaxOpRows || vocab < 1 ? 0 : rows_workspace(rows, vocab, true);
+}
+
+extern "C" dvi_status dvi_policy_loss(const dvi_policy_args *g, void *workspace, size_t ws_bytes, void *hip_stream) {
+    if (!g) return op_fail(DVI_ERR_ARG, "null arguments");
+    dvi_status st = check_rows(g->rows, g->vocab, g->dtype, g->logits, g->ld, g->tokens, g->temperature);
+    if (st != DVI_OK) return st;
+    if (!g->terms) return op_fail(DVI_ERR_ARG, "terms must be given");
+    if (g->rows && !g->advantages) return op_fail(DVI_ERR_ARG, "advantages must be given");
+    if (g->ref_logits && g->ref_logp) return op_fail(DVI_ERR_ARG, "ref_logits and ref_logp exclude each other");
+    if (!(g->clip_low >= 0.0 && g->clip_low <= 1.0) || !(g->clip_high >= 0.0))
+        return op_fail(DVI_ERR_ARG, "0 <= clip_low <= 1 and 0 <= clip_high");
+    if (!isfinite(g->c_kl) || !isfinite(g->c_ent)) return op_fail(DVI_ERR_ARG, "c_kl and c_ent must be finite");
+    if (g->c_kl != 0.0 && !g->ref_logits && !g->ref_logp) return op_fail(DVI_ERR_ARG, "c_kl needs ref_logits or ref_logp");
+    const size_t es = op_size(g->dtype);
+    if (g->ref_logits) {
+        if (!(g->ref_temperature > 0.0) || !(g->ref_temperature < 1e30))
+            return op_fail(DVI_ERR_ARG, "ref_temperature must be > 0 and finite");
+        if (g->ref_ld < 0 || g->ref_ld > kMaxOpStride) return op_fail(DVI_ERR_ARG, "row strides from 0 to 2^36");
+        if ((uintptr_t)g->ref_logits % es) return op_fail(DVI_ERR_ARG, "ref_logits are not aligned to their type");
+    }
+    if (g->grad && g->rows) {
+        if (g->grad_ld < g->vocab || g->grad_ld > kMaxOpStride) return op_fail(DVI_ERR_ARG, "grad_ld from vocab to 2^36");
+        if ((uintptr_t)g->grad % es) return op_fail(DVI_ERR_ARG, "grad is not aligned to its type");
+        const bool same = g->grad == g->logits && (g->grad_ld == g->ld || g->rows == 1);
+        if (!same && !rows_apart(g->grad, g->grad_ld, g->logits, g->ld, g->rows, g->vocab, es))
+            return op_fail(DVI_ERR_ARG, "grad overlaps logits without being the same rows");
+        if (g->ref_logits && !rows_apart(g->grad, g->grad_ld, g->ref_logits, g->ref_ld, g->rows, g->vocab, es))
+            return op_fail(DVI_ERR_ARG, "grad overlaps ref_logits");
+    }
+    st = op_workspace(workspace, ws_bytes, rows_workspace(g->rows, g->vocab, true));
+    if (st != DVI_OK) return st;
+    RowArgs a{};
+    a.z = g->logits;
+    a.ldz = g->ld;
+    a.q = g->ref_logits;
+    a.ldq = g->ref_ld;
+    a.tok = g->tokens;
+    a.N = g->rows;
+    a.V = g->vocab;
+    a.it = 1.0 / g->temperature;
+    a.iq = g->ref_logits ? 1.0 / g->ref_temperature : a.it;
+    a.logp = g->logp;
+    a.policy = 1;
+    a.adv = g->advantages;
+    a.old = g->old_logp;
+    a.weights = g->weights;
+    a.ref_logp = g->ref_logp;
+    a.w0 = g->rows ? (float)(1.0 / (double)g->rows) : 0.f;
+    a.lo = 1.0 - g->clip_low;
+    a.hi = 1.0 + g->clip_high;
+    a.c_kl = g->c_kl;
+    a.c_ent = g->c_ent;
+    a.dz = g->grad;
+    a.lddz = g->grad_ld;
+    a.terms = g->terms;
+    launch_rows(op_dtype(g->dtype), a, workspace, (hipStream_t)hip_stream);
+    return op_launched();
+}
+
+// A launch's threads are counted in 32 bits, 256 of them for a chunk.
+static constexpr int64_t kMaxAdamChunks = (int64_t)1 << 23, kMaxAdamElements = kMaxAdamChunks * kAdamChunk;
+
+static int adam_groups(int n) { return (n + kAdamTensors - 1) / kAdamTensors; }
+
+extern "C" size_t dvi_adamw_workspace_bytes(int32_t n_tensors) {
+    return n_tensors < 0 ? 0 : align_up((size_t)std::max(1, adam_groups(n_tensors)) * kNormGrid * sizeof(double));
+}
+
+// The two keys of a step's random bits: a 64-bit mix of the seed and the step.
+static void step_keys(uint64_t seed, int32_t step, uint32_t &key0, uint32_t &key1) {
+    uint64_t x = seed + (uint64_t)step * 0x9e3779b97f4a7c15ull;
+    x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;
+    x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
+    x ^= x >> 31;
+    key0 = (uint32_t)x;
+    key1 = (uint32_t)(x >> 32);
+}
+
+// What the step makes of its host numbers.
+static AdamArgs adam_numbers(double lr, double beta1, double beta2, double eps, double decay, int32_t step, double max_norm,
+                             uint64_t seed) {
+    AdamArgs a{};
+    a.b1 = (float)beta1;
+    a.one_b1 = (float)(1.0 - beta1);
+    a.b2 = (float)beta2;
+    a.one_b2 = (float)(1.0 - beta2);
+    a.decay = (float)(1.0 - lr * decay);
+    a.rate = (float)(lr / (1.0 - pow(beta1, step)));
+    a.root = (float)(1.0 / sqrt(1.0 - pow(beta2, step)));
+    a.eps = (float)eps;
+    a.max_norm = (float)max_norm;
+    step_keys(seed, step, a.key0, a.key1);
+    return a;
+}
+
+// Up to kAdamTensors of the tensors from `at` on that have elements, with their random bits counted from
+// `base`; moves both on.
+static int adam_group(const dvi_adamw_tensor *tensors, int n_tensors, int &at, long &base, AdamTensor *out) {
+    int n = 0;
+    for (; at < n_tensors && n < kAdamTensors; ++at) {
+        const dvi_adamw_tensor &d = tensors[at];
+        if (d.n == 0) continue;
+        out[n++] = {(long)d.n, d.param, d.master, d.grad, d.m, d.v, d.m_scale, d.v_scale, base};
+        base += (long)((d.n + kStateBlock - 1) / kStateBlock) * kStateBlock;
+    }
+    return n;
+}
+
+// The norm (max_norm > 0) and the step, kAdamTensors tensors a launch.
+static void launch_adam_step(DType pt, bool master, DType gt, int bits, const dvi_adamw_tensor *tensors, int n_tensors,
+                             AdamArgs a, double *part, float *norm, hipStream_t s) {
+    AdamTensor t[kAdamTensors];
+    long base = 0;
+    if (a.max_norm > 0.f) {
+        a.norm_part = part;
+        for (int at = 0, n; (n = adam_group(tensors, n_tensors, at, base, t)) > 0;) {
+            launch_adam_norm(gt, t, n, part + a.n_part, s);
+            a.n_part += adam_norm_parts(t, n);
+        }
+        if (a.n_part == 0 && norm) launch_adam_norm_out(part, 0, norm, s);
+    }
+    a.norm = norm;
+    base = 0;
+    for (int at = 0, n; (n = adam_group(tensors, n_tensors, at, base, t)) > 0; a.norm = nullptr)
+        launch_adamw(pt, master, gt, bits, t, n, a, s);
+}
+
+extern "C" dvi_status dvi_adamw(const dvi_adamw_tensor *tensors, int32_t n_tensors, const dvi_adamw_args *g, void *workspace,
+                                size_t ws_bytes, void *hip_stream) {
+    if (!g || n_tensors < 0 || (n_tensors && !tensors)) return op_fail(DVI_ERR_ARG, "null arguments");
+    if ((g->dtype != DVI_FP32 && g->dtype != DVI_BF16) || (g->grad_dtype != DVI_FP32 && g->grad_dtype != DVI_BF16))
+        return op_fail(DVI_ERR_ARG, "dtypes must be DVI_FP32 or DVI_BF16");
+    if (g->state_bits != 8 && g->state_bits != 32) return op_fail(DVI_ERR_ARG, "state_bits must be 8 or 32");
+    if (g->step < 1) return op_fail(DVI_ERR_ARG, "step must be >= 1");
+    if (!isfinite(g->lr) || !isfinite(g->weight_decay)) return op_fail(DVI_ERR_ARG, "lr and weight_decay must be finite");
+    if (!(g->beta1 >= 0.0 && g->beta1 < 1.0) || !(g->beta2 >= 0.0 && g->beta2 < 1.0))
+        return op_fail(DVI_ERR_ARG, "0 <= beta1, beta2 < 1");
+    if (!(g->eps > 0.0) || !isfinite(g->eps)) return op_fail(DVI_ERR_ARG, "eps must be > 0");
+    if (!(g->max_norm >= 0.0)) return op_fail(DVI_ERR_ARG, "max_norm must not be negative");
+    if (g->grad_norm && g->max_norm == 0.0) return op_fail(DVI_ERR_ARG, "grad_norm needs max_norm > 0");
+    int masters = 0, used = 0;
+    int64_t chunks = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        const dvi_adamw_tensor &d = tensors[i];
+        if (d.n < 0) return op_fail(DVI_ERR_ARG, "tensor %d: negative length", i);
+        if (d.n == 0) continue;
+        if (!d.param || !d.grad || !d.m || !d.v) return op_fail(DVI_ERR_ARG, "tensor %d: null array", i);
+        if (g->state_bits == 8 && (!d.m_scale || !d.v_scale)) return op_fail(DVI_ERR_ARG, "tensor %d: 8-bit states need scales", i);
+        if (d.master && g->dtype != DVI_BF16) return op_fail(DVI_ERR_ARG, "tensor %d: only bf16 parameters have a master", i);
+        const uintptr_t words = (uintptr_t)d.master | (uintptr_t)d.m_scale | (uintptr_t)d.v_scale |
+                                (g->state_bits == 32 ? (uintptr_t)d.m | (uintptr_t)d.v : 0);
+        if ((uintptr_t)d.param % op_size(g->dtype) || (uintptr_t)d.grad % op_size(g->grad_dtype) || words % 4)
+            return op_fail(DVI_ERR_ARG, "tensor %d: an array is not aligned to its type", i);
+        masters += d.master != nullptr;
+        ++used;
+        chunks += d.n > kMaxAdamElements ? kMaxAdamChunks + 1 : (d.n + kAdamChunk - 1) / kAdamChunk;
+        if (chunks > kMaxAdamChunks) return op_fail(DVI_ERR_CAPACITY, "more than 2^35 elements");
+    }
+    if (masters && masters != used) return op_fail(DVI_ERR_ARG, "some tensors have a master and some do not");
+    if (used == 0 && g->max_norm == 0.0) return DVI_OK;
+    const dvi_status st = op_workspace(workspace, ws_bytes, g->max_norm > 0.0 ? dvi_adamw_workspace_bytes(used) : 0);
+    if (st != DVI_OK) return st;
+    launch_adam_step(op_dtype(g->dtype), masters > 0, op_dtype(g->grad_dtype), g->state_bits, tensors, n_tensors,
+                     adam_numbers(g->lr, g->beta1, g->beta2, g->eps, g->weight_decay, g->step, g->max_norm, g->seed),
+                     (double *)workspace, g->grad_norm, (hipStream_t)hip_stream);
+    return op_launched();
 }
 
 // ------------------------------------------------------------------------------------------

@@ -1,0 +1,703 @@
+"""Learning operators (token log-probabilities, clipped policy loss, AdamW) against their definitions in 64 bits.
+
+Tolerances.  u = 2^-24.  A logit's x = (z - M) / T carries a few roundings, so that e^x is off by at most
+(4 |x| + 4) u of itself; a sum over a row adds one rounding for each addition a thread makes in a row and
+for the tree that joins the threads.  tol(R, V) bounds the relative error of a probability with |x| <= R, and
+of a sum of such; it is generous for the chain (V / 256 additions) and tight in what it is relative to:
+every element of a gradient is held to tol times the sum of the magnitudes of its own terms.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+LO, HI = 0.2, 0.28
+
+
+def learn():
+    from paper_2510_05421_amd import learn
+    return learn
+
+
+def tol(R, V):
+    return (8 * R + V / 256 + 48) * U
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2 if dtype == BF16 else 0.0
+
+
+def make_rows(n, V, dtype, seed=0, pad=0, banned=0.0, dead=0.0, temp=1.0, low=-math.inf):
+    g = torch.Generator().manual_seed(seed * 1009 + n * 31 + V)
+    z = torch.randn(n, V + pad, generator=g) * 2.5
+    z[torch.arange(n), torch.randint(0, V, (n,), generator=g)] += 5.0
+    if banned:
+        out = torch.rand(V, generator=g) < banned
+        out[0] = False
+        z[:, :V][:, out] = low
+    buf = z.to(dtype)
+    v = buf[:, :V]
+    tok = torch.multinomial(torch.softmax(v.float() / temp, -1), 1, generator=g)[:, 0].to(torch.int32)
+    if dead:
+        off = torch.rand(n, generator=g) < dead
+        off[0] = False
+        tok[off] = -1
+    return buf.cuda()[:, :V], tok.cuda(), g
+
+
+def make_policy(n, V, dtype, ref, seed=0, **kw):
+    z, tok, g = make_rows(n, V, dtype, seed, **kw)
+    T = kw.get("temp", 1.0)
+    lp = torch.log_softmax(z.cpu().double() / T, -1).gather(1, tok.cpu().clamp(min=0).long()[:, None])[:, 0]
+    moved = torch.randn(n, generator=g, dtype=torch.float64) * 0.2
+    for border in (math.log(1 - LO), math.log(1 + HI)):   # on the border either side is right
+        moved = torch.where((moved - border).abs() < 1e-3, border + 2e-3, moved)
+    d = dict(advantages=torch.randn(n, generator=g), old_logp=(lp - moved).float(),
+             weights=torch.rand(n, generator=g) / n)
+    d["weights"][tok.cpu() < 0] = 0.0
+    if ref == "tokens":
+        d["ref_logp"] = (lp + 0.3 * torch.randn(n, generator=g)).float()
+    elif ref == "logits":
+        d["ref_logits"] = (z.cpu().float() + 0.5 * torch.randn(n, V, generator=g)).to(dtype)
+    return z, tok, {k: v.cuda() for k, v in d.items()}
+
+
+def oracle(z, tok, advantages, old_logp=None, weights=None, ref_logits=None, ref_logp=None, temperature=1.0,
+           ref_temperature=1.0, clip_low=0.2, clip_high=0.2, c_kl=0.0, c_ent=0.0):
+    """The loss and its gradient in 64 bits, and for each element of the gradient the magnitudes it is a sum of."""
+    def f(t):
+        return None if t is None else t.detach().cpu().double()
+
+    z, adv, old, w, q, rlp = f(z), f(advantages), f(old_logp), f(weights), f(ref_logits), f(ref_logp)
+    tok = tok.cpu().long()
+    n, V = z.shape
+    w = torch.full((n,), 1.0 / max(n, 1), dtype=torch.float64) if w is None else w
+    w = w.float().double()
+    live = (tok >= 0) & (tok < V) & (w != 0) & (z > -math.inf).any(-1)
+    if q is not None:
+        live &= (q > -math.inf).any(-1)
+    z = torch.where(live[:, None], z, 0.0)
+    at = tok.clamp(0, V - 1)
+    lg = torch.log_softmax(z / temperature, -1)
+    p = lg.exp()
+    pl = torch.where(p > 0, p * lg, 0.0)
+    H = -pl.sum(-1)
+    lp = lg[torch.arange(n), at]
+    ratio = torch.ones(n, dtype=torch.float64) if old is None else (lp - old).exp()
+    held = ratio.clamp(1 - clip_low, 1 + clip_high)
+    cut = held * adv < ratio * adv
+    pol = torch.where(cut, -held * adv, -ratio * adv)
+    by = torch.where(cut, 0.0, -ratio * adv)
+    by_mag = by.abs()
+    kl = torch.zeros(n, dtype=torch.float64)
+    inner = c_ent * torch.where(p > 0, lg + H[:, None], 0.0)
+    mag = abs(c_ent) * torch.where(p > 0, lg.abs() + H[:, None], 0.0)
+    if rlp is not None:
+        r = rlp - lp
+        kl = r.exp() - r - 1
+        by = by + c_kl * (1 - r.exp())
+        by_mag = by_mag + abs(c_kl) * (1 + r.exp())
+    if q is not None:
+        q = torch.where(live[:, None], q, 0.0)
+        apart = torch.where(p > 0, lg - torch.log_softmax(q / ref_temperature, -1), 0.0)
+        kl = (p * apart).sum(-1)
+        inner = inner + c_kl * (apart - kl[:, None])
+        mag = mag + abs(c_kl) * (2 * (lg.abs() + (lg - apart).abs()) + (p * apart.abs()).sum(-1)[:, None])
+    hot = torch.zeros_like(p)
+    hot[torch.arange(n), at] = 1.0
+    scale = (w / temperature)[:, None]
+    grad = scale * (p * inner + by[:, None] * (hot - p))
+    mag = scale.abs() * (torch.where(p > 0, p * mag, 0.0) + by_mag[:, None] * (hot + p))
+    grad, mag = torch.where(live[:, None], grad, 0.0), torch.where(live[:, None], mag, 0.0)
+    rows = torch.where(live, torch.stack([pol, kl, H, cut.double()]), 0.0)
+    wl = torch.where(live, w, 0.0)
+    sums = (rows * wl).sum(-1)
+    mags = (torch.where(live, torch.stack([pol.abs(), 1 + kl.abs(), 1 + H, cut.double()]), 0.0) * wl.abs()).sum(-1)
+    terms = torch.cat([(sums[0] + c_kl * sums[1] - c_ent * sums[2])[None], sums])
+    tmag = torch.cat([(mags[0] + abs(c_kl) * mags[1] + abs(c_ent) * mags[2])[None], mags])
+    spread = torch.where(p > 1e-30, (lg - lg.amax(-1, keepdim=True)).abs(), 0.0).max().item() if n else 0.0
+    return dict(grad=grad, mag=mag, terms=terms, tmag=tmag, logp=torch.where(live, lp, 0.0),
+                entropy=torch.where(live, H, 0.0), R=spread, live=live)
+
+
+def check_policy(out, want, dtype, V):
+    t = tol(want["R"], V)
+    got = out.grad.cpu().double()
+    assert torch.isfinite(got).all()
+    # a probability below the smallest normal number may be 0
+    off = (got - want["grad"]).abs() - (t * want["mag"] + half_step(dtype) * (want["grad"].abs() + t * want["mag"]) + 1e-37)
+    assert off.max().item() <= 0, "gradient off by %.3g more than %.3g of its terms" % (off.max().item(), t)
+    assert (got[~want["live"]] == 0).all()
+    lp = out.logp.cpu().double()
+    assert ((lp - want["logp"]).abs() <= t + U * want["logp"].abs()).all()
+    te = out.terms.cpu().double()
+    assert ((te - want["terms"]).abs() <= 2 * t * want["tmag"] + 1e-30).all(), (te, want["terms"])
+
+
+SHAPES = [(1, 1), (2, 2), (7, 3), (3, 5), (5, 63), (1, 127), (9, 128), (300, 257), (2, 1000), (16, 4096), (3, 4097),
+          (1, 8191), (300, 8200), (1, 32000), (48, 32000), (5, 33001), (1, 65537), (2, 131072), (1, 150001)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", SHAPES)
+def test_logprobs(n, V, dtype):
+    z, tok, _ = make_rows(n, V, dtype, temp=0.8, dead=0.2)
+    lp, ent = learn().token_logprobs(z, tok, temperature=0.8, entropy=True)
+    want = oracle(z, tok, torch.ones(n), temperature=0.8)
+    t = tol(want["R"], V)
+    assert ((lp.cpu().double() - want["logp"]).abs() <= t + U * want["logp"].abs()).all()
+    assert ((ent.cpu().double() - want["entropy"]).abs() <= t * (1 + want["entropy"]) + U).all()
+    only, none = learn().token_logprobs(z, tok, temperature=0.8)
+    assert none is None and torch.equal(only, lp)
+
+
+@pytest.mark.parametrize("ref", ["none", "tokens", "logits"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", SHAPES)
+def test_policy_loss(n, V, dtype, ref):
+    z, tok, d = make_policy(n, V, dtype, ref, dead=0.2, temp=1.3)
+    kw = dict(temperature=1.3, ref_temperature=0.9, clip_low=LO, clip_high=HI, c_kl=0.0 if ref == "none" else 0.3, c_ent=0.02)
+    out = learn().policy_loss(z, tok, **d, **kw)
+    check_policy(out, oracle(z, tok, **d, **kw), dtype, V)
+    again = learn().policy_loss(z, tok, **d, **kw)
+    assert torch.equal(out.terms, again.terms) and torch.equal(out.grad, again.grad) and torch.equal(out.logp, again.logp)
+    no = learn().policy_loss(z, tok, **d, **kw, grad=False)
+    assert no.grad is None
+    w = oracle(z, tok, **d, **kw)
+    assert ((no.terms.cpu().double() - w["terms"]).abs() <= 2 * tol(w["R"], V) * w["tmag"] + 1e-30).all()
+
+
+@pytest.mark.parametrize("ref", ["none", "tokens", "logits"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V,pad,skip", [(4, 1000, 24, 1), (3, 4099, 6, 3), (2, 32001, 7, 5), (64, 513, 1, 2), (2, 140000, 3, 1)])
+def test_strides_alignments_and_in_place(n, V, pad, skip, dtype, ref):
+    """Rows of a wider buffer that start at any element; the gradient over the logits, and into a buffer
+    of another stride whose other columns stay as they are."""
+    z0, tok, d = make_policy(n, V, dtype, ref)
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.0 if ref == "none" else 0.3, c_ent=0.02)
+    want = oracle(z0, tok, **d, **kw)
+
+    def wide(t, fill):
+        buf = torch.full((n * (V + pad) + skip,), fill, dtype=dtype, device="cuda")
+        v = buf[skip:].view(n, V + pad)[:, :V]
+        v.copy_(t)
+        return buf, v
+
+    _, z = wide(z0, float("nan"))
+    if ref == "logits":
+        d["ref_logits"] = wide(d["ref_logits"], float("nan"))[1]
+    buf, out = wide(torch.zeros_like(z0), 7.0)
+    got = learn().policy_loss(z, tok, **d, **kw, out=out)
+    check_policy(got, want, dtype, V)
+    assert torch.equal(z, z0)
+    rest = buf[skip:].view(n, V + pad)[:, V:]
+    assert (rest == 7.0).all() and (buf[:skip] == 7.0).all()
+    apart = got.grad.clone()
+    place = learn().policy_loss(z, tok, **d, **kw, out=z)
+    assert place.grad.data_ptr() == z.data_ptr() and torch.equal(z, apart) and torch.equal(place.terms, got.terms)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(3, 300), (2, 40000), (300, 1000)])
+@pytest.mark.parametrize("low", ["inf", "lowest"])
+def test_forbidden_tokens(n, V, dtype, low):
+    """Half of the vocabulary at -inf, or at the type's lowest number, in the policy and in the reference."""
+    val = -math.inf if low == "inf" else torch.finfo(dtype).min
+    z, tok, d = make_policy(n, V, dtype, "logits", banned=0.5, low=val)
+    out = z == val
+    d["ref_logits"] = torch.where(out, torch.full_like(z, val), d["ref_logits"])
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.3, c_ent=0.02)
+    want = oracle(z, tok, **d, **kw)
+    got = learn().policy_loss(z, tok, **d, **kw)
+    check_policy(got, want, dtype, V)
+    assert (got.grad[out] == 0).all()
+    # the reference forbids nothing: finite all the same
+    d["ref_logits"] = torch.randn(n, V, device="cuda").to(dtype)
+    check_policy(learn().policy_loss(z, tok, **d, **kw), oracle(z, tok, **d, **kw), dtype, V)
+    # it forbids what the policy may say: the divergence is infinite (beyond any fp32 number or -inf)
+    d["ref_logits"] = torch.full_like(d["ref_logits"], val)
+    d["ref_logits"][:, 0] = 0.0
+    d.pop("old_logp")
+    only = learn().policy_loss(z, tok, **d, **dict(kw, c_kl=0.0))
+    assert only.terms[2].item() > 1e30
+    d.pop("ref_logits")     # reported, it takes no part in the loss
+    check_policy(only._replace(terms=learn().policy_loss(z, tok, **d, **dict(kw, c_kl=0.0)).terms),
+                 oracle(z, tok, **d, **dict(kw, c_kl=0.0)), dtype, V)
+    assert only.terms[0].item() == learn().policy_loss(z, tok, **d, **dict(kw, c_kl=0.0)).terms[0].item()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("ref", ["none", "logits"])
+@pytest.mark.parametrize("V", [37, 4096, 50001])
+def test_rows_that_are_masked(V, ref, dtype):
+    """Weight 0, a token outside the vocabulary, no logit above -inf (there or in the reference): nothing
+    else of the row is looked at, and its gradient is 0.  A row of equal lowest numbers is a row."""
+    n = 8
+    z, tok, d = make_policy(n, V, dtype, ref, seed=3)
+    d["weights"].fill_(0.1)
+    lowest = torch.finfo(dtype).min
+    d["weights"][0] = 0.0
+    z[0] = float("nan")
+    d["old_logp"][0] = d["advantages"][0] = float("nan")
+    tok[1] = -1
+    z[1] = float("inf")
+    tok[2] = V
+    tok[3] = torch.iinfo(torch.int32).min
+    z[4] = -math.inf
+    z[5] = lowest
+    d["old_logp"][5] = -math.log(V)
+    if ref == "logits":
+        d["ref_logits"][6] = -math.inf
+        d["ref_logits"][0] = float("nan")
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.0 if ref == "none" else 0.3, c_ent=0.02)
+    want = oracle(z, tok, **d, **kw)
+    assert want["live"].tolist() == [False] * 5 + [True, ref == "none", True]
+    got = learn().policy_loss(z, tok, **d, **kw)
+    check_policy(got, want, dtype, V)
+    assert (got.logp[:5] == 0).all()
+    lp, ent = learn().token_logprobs(z, tok, entropy=True)
+    assert (lp[1:5] == 0).all() and (ent[1:5] == 0).all()
+    assert abs(lp[5].item() + math.log(V)) <= tol(0, V) + U * math.log(V)
+    assert abs(ent[5].item() - math.log(V)) <= tol(0, V) * (1 + math.log(V))
+    # all rows masked
+    d["weights"].zero_()
+    none = learn().policy_loss(z, tok, **d, **kw)
+    assert (none.grad == 0).all() and (none.terms == 0).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("V", [100, 40000])
+def test_numbers_that_are_not_finite_show(bad, V):
+    z, tok, d = make_policy(3, V, F32, "none")
+    z[1, V // 2] = bad
+    got = learn().policy_loss(z, tok, **d)
+    assert torch.isnan(got.terms[0]) and torch.isnan(got.logp[1])
+    assert torch.isfinite(got.grad[0]).all() and torch.isfinite(got.grad[2]).all()
+    lp, ent = learn().token_logprobs(z, tok, entropy=True)
+    assert torch.isnan(lp[1]) and torch.isnan(ent[1]) and torch.isfinite(lp[0]) and torch.isfinite(lp[2])
+
+
+def test_no_rows():
+    z = torch.empty(0, 50, device="cuda")
+    e, tok = torch.empty(0, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    got = learn().policy_loss(z, tok, e)
+    assert got.grad.shape == (0, 50) and (got.terms == 0).all()
+    assert learn().token_logprobs(z, tok)[0].shape == (0,)
+
+
+def test_defaults_are_the_plain_policy_gradient():
+    """No old log-probabilities: ratio 1; no weights: 1 / rows."""
+    z, tok, d = make_policy(6, 500, F32, "none")
+    got = learn().policy_loss(z, tok, d["advantages"])
+    check_policy(got, oracle(z, tok, d["advantages"]), F32, 500)
+    assert got.terms[4].item() == 0 and abs(got.loss.item() + d["advantages"].mean().item()) <= 1e-6
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_expanded_rows(dtype):
+    """One row of reference logits, and one of logits, for all rows (stride 0); the gradient of each is whole."""
+    z, tok, d = make_policy(5, 700, dtype, "logits")
+    d["ref_logits"] = d["ref_logits"][:1].expand(5, 700)
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.3, c_ent=0.02)
+    check_policy(learn().policy_loss(z, tok, **d, **kw), oracle(z, tok, **d, **kw), dtype, 700)
+    z1 = z[:1].expand(5, 700)
+    check_policy(learn().policy_loss(z1, tok, **d, **kw), oracle(z1, tok, **d, **kw), dtype, 700)
+
+
+@pytest.mark.parametrize("ref", ["none", "tokens", "logits"])
+def test_gradient_against_differences(ref):
+    """Central differences of the loss the kernel itself computes.  With a step of 2^-4 the third derivative
+    of these losses (below 4 times the largest first one) leaves 2^-8 / 6 * 4 = 2.6e-3 of it, and the loss's
+    rounding 2 tol / 2^-4."""
+    n, V, h = 3, 12, 2.0 ** -4
+    z, tok, d = make_policy(n, V, F32, ref, seed=5)
+    z = z * 0.4
+    lp = torch.log_softmax(z.double(), -1).gather(1, tok.long()[:, None])[:, 0]
+    d["old_logp"] = (lp - torch.tensor([0.05, -0.05, 0.0], device="cuda")).float()   # inside the borders
+    d["weights"] = torch.tensor([0.5, 0.2, 0.3], device="cuda")
+    kw = dict(clip_low=0.9, clip_high=5.0, c_kl=0.0 if ref == "none" else 0.3, c_ent=0.05)
+    g = learn().policy_loss(z, tok, **d, **kw).grad.cpu().double()
+    big = g.abs().max().item()
+    for i in range(n):
+        for j in range(V):
+            up, down = z.clone(), z.clone()
+            up[i, j] += h
+            down[i, j] -= h
+            diff = (learn().policy_loss(up, tok, **d, **kw, grad=False).loss.double()
+                    - learn().policy_loss(down, tok, **d, **kw, grad=False).loss.double()).item() / (2 * h)
+            assert abs(diff - g[i, j].item()) <= 2.6e-3 * max(big, 0.1) + tol(4, V) * 4 / h
+
+
+def test_large_offsets():
+    """A buffer whose rows lie more than 2^32 bytes apart."""
+    ld, V = (1 << 31) + 4096, 1000
+    z0, tok, d = make_policy(2, V, BF16, "tokens", seed=7)
+    buf = torch.empty(ld + V, dtype=BF16, device="cuda")
+    z = torch.as_strided(buf, (2, V), (ld, 1))
+    z.copy_(z0)
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.3, c_ent=0.02)
+    want = oracle(z0, tok, **d, **kw)
+    check_policy(learn().policy_loss(z, tok, **d, **kw), want, BF16, V)
+    check_policy(learn().policy_loss(z, tok, **d, **kw, out=z), want, BF16, V)
+
+
+@pytest.mark.parametrize("n,V", [(2, 70000), (300, 700)])
+def test_captured_and_on_other_streams(n, V):
+    z, tok, d = make_policy(n, V, F32, "logits")
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.3, c_ent=0.02)
+    want = learn().policy_loss(z, tok, **d, **kw)
+    lp_want = learn().token_logprobs(z, tok)[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = learn().policy_loss(z, tok, **d, **kw)
+    other = learn().policy_loss(z, tok, **d, **kw)      # both in flight
+    torch.cuda.synchronize()
+    for o in (got, other):
+        assert torch.equal(o.grad, want.grad) and torch.equal(o.terms, want.terms)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cap = learn().policy_loss(z, tok, **d, **kw)
+        lp = learn().token_logprobs(z, tok)[0]
+    second = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(second):
+        cap2 = learn().policy_loss(z, tok, **d, **kw)
+    for k in range(4):
+        for o in (cap, cap2):
+            o.grad.fill_(float("nan"))
+            o.terms.fill_(float("nan"))
+        lp.fill_(float("nan"))
+        graph.replay()
+        second.replay()
+        eager = learn().policy_loss(z, tok, **d, **kw)
+        torch.cuda.synchronize()
+        for o in (cap, cap2, eager):
+            assert torch.equal(o.grad, want.grad) and torch.equal(o.terms, want.terms) and torch.equal(o.logp, want.logp), k
+        assert torch.equal(lp, lp_want)
+
+
+def test_binding_refuses():
+    from paper_2510_05421_amd._abi import DVIError
+    L = learn()
+    z, tok, d = make_policy(4, 64, F32, "logits")
+    bad = [dict(logits=z.cpu()), dict(logits=z.half()), dict(logits=z[0]), dict(logits=z.t()[:4, :4].t()[:, ::2]),
+           dict(tokens=tok.long()), dict(tokens=tok[:3]), dict(tokens=tok.cpu()), dict(advantages=None),
+           dict(advantages=d["advantages"].double()), dict(advantages=torch.zeros(8, device="cuda")[::2]),
+           dict(weights=d["weights"].cpu()), dict(ref_logits=d["ref_logits"].to(BF16)), dict(ref_logits=d["ref_logits"][:, :32]),
+           dict(ref_logp=d["old_logp"]), dict(out=torch.empty(4, 64, dtype=BF16, device="cuda")),
+           dict(out=torch.empty(4, 65, device="cuda")), dict(out=torch.zeros(4, 64, device="cuda"), grad=False),
+           dict(out=torch.empty(1, 64, device="cuda").expand(4, 64)), dict(clip_low=2.0), dict(temperature=0.0),
+           dict(out=d["ref_logits"])]
+    for kw in bad:
+        with pytest.raises(DVIError):
+            L.policy_loss(**dict(dict(logits=z, tokens=tok, **d), **kw))
+    flat = torch.zeros(400, device="cuda")
+    with pytest.raises(DVIError):     # rows that meet the logits' without being them
+        L.policy_loss(flat[:256].view(4, 64), tok, d["advantages"], out=flat[32:288].view(4, 64))
+    with pytest.raises(DVIError):
+        L.token_logprobs(z, tok, temperature=-1.0)
+    p = torch.zeros(300, device="cuda")
+    for args, kw in [([[]], {}), ([[p.half()]], {}), ([[p.cpu()]], {}), ([[p, p]], {}), ([[p[:200], p[100:]]], {}),
+                     ([[p[::2]]], {}), ([[p, torch.zeros(3, dtype=BF16, device="cuda")]], {}), ([[p]], dict(state_bits=4)),
+                     ([[p]], dict(states={"m": [p.clone()]})),
+                     ([[p]], dict(states={"m": [p.clone()], "v": [p[:5].clone()]})),
+                     ([[p]], dict(states={"m": [p], "v": [p.clone()]}))]:
+        with pytest.raises(DVIError):
+            L.AdamW(*args, **kw)
+    opt = L.AdamW([p])
+    for grads in ([], [p.half()], [p[:10]], [p.cpu()], [torch.zeros(600, device="cuda")[::2]]):
+        with pytest.raises(DVIError):
+            opt.step(grads)
+    for kw in (dict(lr=float("nan")), dict(betas=(0.9, 1.0)), dict(eps=0.0), dict(max_norm=-1.0)):
+        with pytest.raises(DVIError):
+            L.AdamW([p], **kw).step([torch.zeros(300, device="cuda")])
+
+
+# ------------------------------------------------------------------ AdamW
+SIZES = [1, 0, 3, 255, 256, 257, 1023, 4095, 4096, 4097, 12288 + 100, 2, 70001]
+
+
+def adam_oracle(p, g, m, v, step, lr, b1, b2, eps, wd, max_norm):
+    """Lists of 64-bit tensors: one step."""
+    norm = math.sqrt(sum(float((x * x).sum()) for x in g))
+    clip = min(1.0, max_norm / norm) if max_norm > 0 and norm > 0 else 1.0
+    out = [], [], []
+    for pi, gi, mi, vi in zip(p, g, m, v):
+        gi = gi * clip
+        mi, vi = b1 * mi + (1 - b1) * gi, b2 * vi + (1 - b2) * gi * gi
+        pi = pi - lr * wd * pi - lr * (mi / (1 - b1 ** step)) / ((vi / (1 - b2 ** step)).sqrt() + eps)
+        for o, x in zip(out, (pi, mi, vi)):
+            o.append(x)
+    return (*out, norm)
+
+
+def adam_inputs(sizes, dtype, gdtype, seed=0, gstd=0.01, skip=0):
+    g = torch.Generator().manual_seed(seed)
+    params = [torch.cat([torch.zeros(skip), torch.randn(s, generator=g)]).to(dtype).cuda()[skip:] for s in sizes]
+    grads = [[torch.cat([torch.zeros(skip), torch.randn(s, generator=g) * gstd]).to(gdtype).cuda()[skip:] for s in sizes]
+             for _ in range(4)]
+    return params, grads
+
+
+def dbl(ts):
+    return [t.detach().cpu().double() for t in ts]
+
+
+@pytest.mark.parametrize("dtype,gdtype,master", [(F32, F32, False), (F32, BF16, False), (BF16, BF16, True), (BF16, F32, True),
+                                                 (BF16, BF16, False), (BF16, F32, False)])
+@pytest.mark.parametrize("max_norm", [0.0, 0.5, 1e9])
+@pytest.mark.parametrize("skip", [0, 1, 3])
+def test_adamw_32bit(dtype, gdtype, master, max_norm, skip):
+    """Four steps, tensors of every awkward size, at any element alignment.  A step's own error: m and v
+    take three roundings each, the quotient about six and p three, so a step moves p by at most 16 u of
+    its change and 3 u of |p| away; clipping adds two roundings to the gradient (u each)."""
+    lr, b1, b2, eps, wd = 1e-2, 0.9, 0.99, 1e-8, 0.1
+    params, grads = adam_inputs(SIZES, dtype, gdtype, skip=skip)
+    opt = learn().AdamW(params, lr=lr, betas=(b1, b2), eps=eps, weight_decay=wd, max_norm=max_norm, master=master)
+    p, m, v = dbl(params), [torch.zeros(s, dtype=torch.float64) for s in SIZES], [torch.zeros(s, dtype=torch.float64) for s in SIZES]
+    for k in range(4):
+        start = dbl(params)
+        opt.step(grads[k])
+        if dtype == BF16 and not master:
+            p = start      # every step starts from the rounded parameter
+        p, m, v, norm = adam_oracle(p, dbl(grads[k]), m, v, k + 1, lr, b1, b2, eps, wd, max_norm)
+        if max_norm:
+            assert abs(opt.grad_norm.item() - norm) <= 2 * U * norm
+        n = k + 1
+        for i, s in enumerate(SIZES):
+            if s == 0:
+                continue
+            gm = max(float(x[i].abs().max()) for x in grads[:n]) if s else 0.0
+            assert ((opt.states["m"][i].cpu().double() - m[i]).abs() <= 8 * n * U * gm).all()
+            assert ((opt.states["v"][i].cpu().double() - v[i]).abs() <= 12 * n * U * v[i] + 1e-37).all()
+            got = (opt.states["master"][i] if master else params[i]).cpu().double()
+            change = lr * 4       # |m| / sqrt(v) of so few steps, bias corrections included, is below 4
+            off = (got - p[i]).abs() - n * (24 * U * change + 4 * U * (p[i].abs() + change))
+            off -= half_step(dtype) * (p[i].abs() + change) if dtype == BF16 and not master else 0.0
+            assert off.max().item() <= 0, (k, s, off.max().item())
+            if master:
+                assert torch.equal(params[i], opt.states["master"][i].to(BF16))
+
+
+@pytest.mark.parametrize("count", [1, 47, 48, 49, 100, 145])
+def test_adamw_many_tensors(count):
+    """More tensors than one launch takes, empty ones among them; one norm over all of them."""
+    sizes = [(i * 37) % 300 + (5000 if i % 17 == 0 else 0) for i in range(count)]
+    if count == 1:
+        sizes = [7]
+    params, grads = adam_inputs(sizes, F32, F32, seed=count)
+    opt = learn().AdamW(params, lr=1e-2, max_norm=0.1)
+    p, m = dbl(params), [torch.zeros(s, dtype=torch.float64) for s in sizes]
+    opt.step(grads[0])
+    p, m, v, norm = adam_oracle(p, dbl(grads[0]), m, m, 1, 1e-2, 0.9, 0.999, 1e-8, 0.0, 0.1)
+    assert abs(opt.grad_norm.item() - norm) <= 2 * U * norm
+    for i in range(count):
+        assert ((params[i].cpu().double() - p[i]).abs() <= 24 * U * 0.02 + 4 * U * p[i].abs()).all()
+
+
+def codes(states, i, n, name):
+    s = states[name + "_scale"][i].cpu().double().repeat_interleave(256)[:n]
+    return states[name][i].cpu().to(torch.float32).double() * s
+
+
+def spacing(x, scale):
+    """Spacing of e4m3 times scale at |x|, upwards."""
+    y = (x.abs() / scale.clamp(min=1e-300)).clamp(min=2.0 ** -6)
+    return 2.0 ** (torch.floor(torch.log2(y)) - 3) * scale
+
+
+@pytest.mark.parametrize("dtype,gdtype,master", [(F32, F32, False), (F32, BF16, False), (BF16, BF16, True), (BF16, F32, True),
+                                                 (BF16, BF16, False), (BF16, F32, False)])
+@pytest.mark.parametrize("max_norm", [0.0, 0.5])
+@pytest.mark.parametrize("skip", [0, 3])
+def test_adamw_8bit(dtype, gdtype, master, max_norm, skip):
+    """Each step against the step in 64 bits from the states as they are held: the parameter to the step's
+    roundings, the new states within one spacing of e4m3 of the exact ones, scales to two roundings.  The two
+    terms of m may cancel, and their roundings (of b1 m0, dequantised with one more, of (1 - b1) g, and of
+    the sum) do not: all of the step's roundings are relative to lr (b1 |m0| + (1 - b1) |g|) / root, not to
+    the step."""
+    lr, b1, b2, eps, wd = 1e-2, 0.9, 0.99, 1e-8, 0.1
+    params, grads = adam_inputs(SIZES, dtype, gdtype, skip=skip)
+    opt = learn().AdamW(params, lr=lr, betas=(b1, b2), eps=eps, weight_decay=wd, max_norm=max_norm, state_bits=8, seed=11,
+                        master=master)
+    for k in range(4):
+        p0 = dbl(opt.states["master"] if master else params)
+        m0 = [codes(opt.states, i, s, "m") for i, s in enumerate(SIZES)]
+        v0 = [codes(opt.states, i, s, "r") ** 2 for i, s in enumerate(SIZES)]
+        opt.step(grads[k])
+        p, m, v, _ = adam_oracle(p0, dbl(grads[k]), m0, v0, k + 1, lr, b1, b2, eps, wd, max_norm)
+        for i, s in enumerate(SIZES):
+            if s == 0:
+                continue
+            got = (opt.states["master"][i] if master else params[i]).cpu().double()
+            terms = b1 * m0[i].abs() + (1 - b1) * grads[k][i].cpu().double().abs()
+            terms = lr * terms / (1 - b1 ** (k + 1)) / ((v[i] / (1 - b2 ** (k + 1))).sqrt() + eps)
+            off = (got - p[i]).abs() - 32 * U * (lr * wd * p0[i].abs() + terms) - 4 * U * p0[i].abs()
+            off -= half_step(dtype) * p[i].abs() * (1 + 1e-3) if dtype == BF16 and not master else 0.0
+            assert off.max().item() <= 0, (k, s)
+            for name, x in (("m", m[i]), ("r", v[i].sqrt())):
+                pad = torch.cat([x.abs(), torch.zeros(-s % 256, dtype=torch.float64)]).view(-1, 256).amax(1) / 448
+                sc = opt.states[name + "_scale"][i].cpu().double()
+                assert ((sc - pad).abs() <= 16 * U * pad).all()
+                sc = sc.repeat_interleave(256)[:s]
+                held = codes(opt.states, i, s, name)
+                assert torch.isfinite(held).all()
+                assert ((held - x).abs() <= spacing(x, sc) * (1 + 1e-4)).all(), (k, s, name)
+                if name == "r":
+                    assert (held[x > 0] > 0).all()
+
+
+def test_adamw_8bit_rounds_with_the_exact_mean():
+    """The mean over many seeds of one state's rounding: the standard error of 1024 throws of at most half a
+    spacing is 1/64 of it, held to five of them, on 2000 elements that share a handful of spacings."""
+    n, seeds = 2000, 1024
+    g = torch.randn(n, generator=torch.Generator().manual_seed(1)).mul_(0.01).cuda()
+    total = {"m": torch.zeros(n, dtype=torch.float64, device="cuda"), "r": torch.zeros(n, dtype=torch.float64, device="cuda")}
+    for s in range(seeds):
+        opt = learn().AdamW([torch.zeros(n, device="cuda")], state_bits=8, seed=s)
+        opt.step([g])
+        for k in total:
+            total[k] += opt.states[k][0].double() * opt.states[k + "_scale"][0].double().repeat_interleave(256)[:n]
+    for k, x in (("m", 0.1 * g.double()), ("r", math.sqrt(0.001) * g.double().abs())):
+        sc = opt.states[k + "_scale"][0].double().repeat_interleave(256)[:n]
+        gap = spacing(x, sc)
+        keep = x.abs() / sc > 2.0 ** -8     # the smallest roots are kept from 0
+        off = ((total[k] / seeds - x).abs() / gap)[keep]
+        assert off.max().item() <= 5 / 64, off.max().item()
+
+
+def test_adamw_8bit_moments_follow_the_gradients():
+    """sqrt(v) of constant gradients after 3000 steps: a rounding to nearest would have stopped it early.
+    Hopping between two codes adds at most half a squared spacing (1/128 of v) to the mean of v, so the mean
+    of sqrt(v) is within 1/128, and an element within two spacings (a quarter)."""
+    n = 4096
+    g = (torch.rand(n, generator=torch.Generator().manual_seed(2)) * 0.9 + 0.1).cuda()
+    opt = learn().AdamW([torch.zeros(n, device="cuda")], lr=0.0, state_bits=8, seed=5)
+    for _ in range(3000):
+        opt.step([g])
+    r = opt.states["r"][0].double() * opt.states["r_scale"][0].double().repeat_interleave(256)
+    ratio = r / (g.double() * math.sqrt(1 - 0.999 ** 3000))
+    assert abs(ratio.mean().item() - 1) <= 1 / 128 + 5 * 0.125 / math.sqrt(n)
+    assert (ratio - 1).abs().max().item() <= 0.25
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_norm_that_is_not_finite_skips_the_step(bits, bad):
+    params, grads = adam_inputs(SIZES, F32, F32)
+    opt = learn().AdamW(params, lr=0.1, weight_decay=0.1, max_norm=1.0, state_bits=bits)
+    opt.step(grads[0])
+    torch.cuda.synchronize()
+    before = [t.clone() for t in params] + [t.clone().view(torch.uint8) for v in opt.states.values() for t in v]
+    grads[1][-1][12345] = bad
+    opt.step(grads[1])
+    after = params + [t.view(torch.uint8) for v in opt.states.values() for t in v]
+    assert all(torch.equal(a, b) for a, b in zip(before, after))
+    assert not math.isfinite(opt.grad_norm.item())
+    opt.step(grads[2])
+    assert math.isfinite(opt.grad_norm.item()) and not torch.equal(params[-1], before[len(SIZES) - 1])
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_zero_gradients_and_states(bits):
+    """Nothing but the decay moves, states stay zero, and no 0 / 0 shows."""
+    p = torch.randn(1000, device="cuda")
+    want = p.double() * (1 - 0.1 * 0.5)
+    opt = learn().AdamW([p], lr=0.1, weight_decay=0.5, max_norm=1.0, state_bits=bits)
+    opt.step([torch.zeros(1000, device="cuda")])
+    assert ((p.double() - want).abs() <= 3 * U * want.abs()).all() and opt.grad_norm.item() == 0.0
+    assert all((t.float() == 0).all() for v in opt.states.values() for t in v)
+    tiny = torch.full((1000,), 1e-32, device="cuda")
+    opt.step([tiny])
+    assert torch.isfinite(p).all() and all(torch.isfinite(t.float()).all() for v in opt.states.values() for t in v)
+
+
+def test_adamw_large_gradients_have_a_norm():
+    """Squares beyond fp32's range: the norm is a sum in 64 bits."""
+    g = torch.full((5000,), 1e25, device="cuda")
+    p = torch.zeros(5000, device="cuda")
+    opt = learn().AdamW([p], lr=0.1, max_norm=1.0)
+    opt.step([g])
+    norm = 1e25 * math.sqrt(5000)
+    assert abs(opt.grad_norm.item() / norm - 1) <= 4 * U
+    assert ((p + 0.1).abs() <= 1e-5).all()       # the first step of Adam is lr, up to eps / |g| = 1e-8 sqrt(5000)
+
+
+def test_adamw_without_some_gradients_and_resumed():
+    params, grads = adam_inputs([500, 300, 700], F32, F32)
+    kept = params[1].clone()
+    opt = learn().AdamW(params, lr=0.1, max_norm=1.0, state_bits=8, seed=3)
+    opt.step([grads[0][0], None, grads[0][2]])
+    assert torch.equal(params[1], kept) and (opt.states["m"][1].float() == 0).all()
+    norm = math.sqrt(sum(float(grads[0][i].double().square().sum()) for i in (0, 2)))
+    assert abs(opt.grad_norm.item() - norm) <= 2 * U * norm
+    copies = [p.clone() for p in params]
+    again = learn().AdamW(copies, lr=0.1, max_norm=1.0, state_bits=8, seed=3, step_count=opt.step_count,
+                          states={k: [t.clone() for t in v] for k, v in opt.states.items()})
+    for o in (opt, again):
+        o.step(grads[1])
+    assert all(torch.equal(a, b) for a, b in zip(params, copies))
+    opt.step([None, None, None])
+    assert all(torch.equal(a, b) for a, b in zip(params, copies)) and opt.grad_norm.item() == 0.0
+
+
+def test_adamw_captured():
+    """A captured step replays with its number; states and parameters move on."""
+    params, grads = adam_inputs([5000, 300], F32, F32)
+    copies = [p.clone() for p in params]
+    opt = learn().AdamW(params, lr=0.01, max_norm=0.5)
+    plain = learn().AdamW(copies, lr=0.01, max_norm=0.5)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step(grads[0])
+    for k in range(4):
+        graph.replay()
+        plain.step_count = 0
+        plain.step(grads[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(params, copies)), k
+        assert torch.equal(opt.grad_norm, plain.grad_norm)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_policy_trains_through_all_of_them(bits):
+    """Behaviour log-probabilities, then three epochs of loss, gradient and step on the two factors of a
+    low-rank head, against the same in 64 bits (states of 8 bits go their own way after the first step)."""
+    L = learn()
+    g = torch.Generator().manual_seed(9)
+    n, V, d, r = 64, 1000, 32, 4
+    h, W = torch.randn(n, d, generator=g), torch.randn(V, d, generator=g) * 0.3
+    A, B = torch.randn(V, r, generator=g) * 0.05, torch.randn(r, d, generator=g) * 0.1
+    tok = torch.randint(0, V, (n,), generator=g).to(torch.int32)
+    adv = torch.randn(n, generator=g)
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.05, c_ent=0.01)
+    hc, Wc, Ac, Bc, tc, ac = (t.cuda() for t in (h, W, A.clone(), B.clone(), tok, adv))
+
+    def logits(h, W, A, B):
+        return h @ W.t() + (h @ B.t()) @ A.t()
+
+    ref = logits(hc, Wc, Ac, Bc)
+    old, _ = L.token_logprobs(ref, tc)
+    opt = L.AdamW([Ac, Bc], lr=2e-3, weight_decay=0.01, max_norm=1.0, state_bits=bits)
+    h64, W64, A64, B64 = h.double(), W.double(), A.double(), B.double()
+    ref64 = logits(h64, W64, A64, B64)
+    old64 = oracle(ref64, tok, adv)["logp"]
+    m, v = [torch.zeros_like(A64), torch.zeros_like(B64)], [torch.zeros_like(A64), torch.zeros_like(B64)]
+    for k in range(3 if bits == 32 else 1):
+        out = L.policy_loss(logits(hc, Wc, Ac, Bc), tc, ac, old, ref_logits=ref, **kw)
+        opt.step([out.grad.t() @ (hc @ Bc.t()), ((out.grad @ Ac).t() @ hc).contiguous()])
+        o = oracle(logits(h64, W64, A64, B64), tok, adv, old64, ref_logits=ref64, **kw)
+        gr = o["grad"]
+        (A64, B64), m, v, _ = adam_oracle([A64, B64], [gr.t() @ (h64 @ B64.t()), (gr @ A64).t() @ h64], m, v, k + 1, 2e-3, 0.9,
+                                          0.999, 1e-8, 0.01, 1.0)
+    # a step is lr m / (sqrt(v) + eps): where a gradient is as small as its own rounding (fp32 products,
+    # about 1e-6 of their terms) the quotient is anything up to 1, so parameters are held in the mean
+    for got, want, start in ((Ac, A64, A), (Bc, B64, B)):
+        off = (got.cpu().double() - want).norm() / (want - start.double()).norm()
+        assert off <= 2e-3, off
+    assert torch.isfinite(L.policy_loss(logits(hc, Wc, Ac, Bc), tc, ac, old, ref_logits=ref, **kw).grad).all()
