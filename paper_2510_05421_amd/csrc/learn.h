@@ -8,8 +8,8 @@
 
 namespace dvi {
 
-// What the kernels keep of a part of a row: with x = (z - M) / T and y = (ref - Mq) / Tr,
-// s = sum e^x, t = sum e^x x, k = sum e^x (x - y), sq = sum e^y; za: the token's logit, where the part
+// What the kernels keep of a part of a row: with x = (z - M) log2(e) / T and y = (ref - Mq) log2(e) / Tr,
+// s = sum 2^x, t = sum 2^x x, k = sum 2^x (x - y), sq = sum 2^y; za: the token's logit, where the part
 // holds it.  M and Mq start at the lowest finite number, so s == 0 says that there is no logit above -inf.
 struct RowStats {
     float M, s, t, k, Mq, sq, za, pad;
@@ -24,6 +24,7 @@ struct RowArgs {
     long N;
     int V;
     double it, iq;           // 1 / T, 1 / Tr
+    float kz, kq;            // log2(e) / T, log2(e) / Tr (set by launch_rows)
     float *logp, *entropy;   // [N] out, or nullptr
     // policy loss (policy != 0)
     int policy;

@@ -69,6 +69,7 @@ template <DType T> struct Chunk {
 template <> struct Chunk<DType::F32> {
     typedef float E;
     static constexpr int N = 4;
+    static constexpr uint32_t kNegInf = 0xff800000u;
     static __device__ __forceinline__ uint4 load(const float *row, int c, int V) {
         uint4 r;
         if ((c + 1) * 4 <= V) {
@@ -93,7 +94,6 @@ template <> struct Chunk<DType::F32> {
 };
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kLog2e = 1.44269504088896341f;
 
 // Whether row i takes part: a weight other than 0 and a token of the vocabulary.
 __device__ __forceinline__ bool row_counts(const RowArgs &a, long i) {
@@ -101,41 +101,47 @@ __device__ __forceinline__ bool row_counts(const RowArgs &a, long i) {
     return t < (uint32_t)a.V && !(a.weights != nullptr && a.weights[i] == 0.f);
 }
 
-// The sums of one more chunk.  With x = (z - M) / T the terms are e^x, e^x x and, for the KL divergence,
-// e^x (x - y): differences of logits that are already relative to their maxima, so nothing large cancels.
-// A -inf (e^x == 0) adds nothing even where x or y is infinite; a NaN makes the sums NaN.
+// a * b with 0 * anything == 0: a probability of 0 takes no part, whatever it is multiplied with.
+// (The compiler has to know the instruction: it keeps a product that follows an exponential of its wave at
+// the distance the hardware needs.)
+__device__ float fmul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float mul0(float a, float b) { return fmul_legacy(a, b); }
+
+// The sums of one more chunk.  x = (z - M) log2(e) / T and y of the reference likewise (kz, kq: log2(e) over
+// the temperature); the terms are 2^x, 2^x x and, for the KL divergence, 2^x (x - y): differences of logits
+// that are already relative to their maxima, so nothing large cancels.  A -inf (2^x == 0) adds nothing even
+// where x or y is infinite; a NaN makes the sums NaN.
 template <DType T, bool REF>
-__device__ __forceinline__ void add_chunk(RowStats &r, const uint4 &zc, const uint4 &qc, float it, float iq) {
+__device__ __forceinline__ void add_chunk(RowStats &r, const uint4 &zc, const uint4 &qc, float kz, float kq) {
     constexpr int N = Chunk<T>::N;
     float z[N], q[N];
     unpack_frag<T>(zc, z);
     if (REF) unpack_frag<T>(qc, q);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float x = (z[k] - r.M) * it, e = __builtin_amdgcn_exp2f(x * kLog2e);
-        const float xc = fmaxf(x, -1e4f);
+        const float x = (z[k] - r.M) * kz, e = __builtin_amdgcn_exp2f(x);
         r.s += e;
-        r.t += e * xc;
+        r.t += mul0(e, x);
         if (REF) {
-            const float y = (q[k] - r.Mq) * iq;
-            r.sq += __builtin_amdgcn_exp2f(y * kLog2e);
-            r.k += e == 0.f ? 0.f : e * (xc - y);
+            const float y = (q[k] - r.Mq) * kq;
+            r.sq += __builtin_amdgcn_exp2f(y);
+            r.k += mul0(e, x - y);
         }
     }
 }
 
 // Sums relative to new maxima M, Mq (at least the old ones).
 template <bool REF>
-__device__ __forceinline__ void rebase(RowStats &r, float M, float Mq, float it, float iq) {
-    const float dx = fmaxf((r.M - M) * it, -1e4f), f = __builtin_amdgcn_exp2f(dx * kLog2e);
+__device__ __forceinline__ void rebase(RowStats &r, float M, float Mq, float kz, float kq) {
+    const float dx = (r.M - M) * kz, f = __builtin_amdgcn_exp2f(dx);
     if (REF) {
-        // a reference masked by the lowest number: dy is as large as that, and counts only where f does
-        const float dy = fmaxf((r.Mq - Mq) * iq, kLowest);
-        r.k = f == 0.f ? 0.f : f * (r.k + (dx - dy) * r.s);
-        r.sq *= __builtin_amdgcn_exp2f(dy * kLog2e);
+        // a reference masked by the lowest number: dy is as large as that, and counts only where f s does
+        const float dy = (r.Mq - Mq) * kq;
+        r.k = mul0(f, r.k + mul0(r.s, dx - dy));
+        r.sq *= __builtin_amdgcn_exp2f(dy);
         r.Mq = Mq;
     }
-    r.t = f * (r.t + dx * r.s);
+    r.t = mul0(f, r.t + mul0(r.s, dx));
     r.s *= f;
     r.M = M;
 }
@@ -167,7 +173,7 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(RowArgs a, int S
     const E *q = REF ? (const E *)a.q + i * a.ldq : nullptr;
     const int nch = (a.V + Chunk<T>::N - 1) / Chunk<T>::N;
     const int c1 = min(nch, (p + 1) * per);
-    const float it = (float)a.it, iq = (float)a.iq;
+    const float kz = a.kz, kq = a.kq;
     RowStats r = {kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, 0.f, 0.f};
     for (int c = p * per + threadIdx.x; c < c1; c += kRowThreads * kRowUnroll) {
         uint4 zc[kRowUnroll], qc[kRowUnroll];
@@ -184,12 +190,12 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(RowArgs a, int S
             M = fmaxf(M, chunk_max<T>(zc[u]));
             if (REF) Mq = fmaxf(Mq, chunk_max<T>(qc[u]));
         }
-        rebase<REF>(r, M, Mq, it, iq);
+        rebase<REF>(r, M, Mq, kz, kq);
 #pragma unroll
         for (int u = 0; u < kRowUnroll; ++u)
-            if (c + u * kRowThreads < c1) add_chunk<T, REF>(r, zc[u], REF ? qc[u] : zc[u], it, iq);
+            if (c + u * kRowThreads < c1) add_chunk<T, REF>(r, zc[u], REF ? qc[u] : zc[u], kz, kq);
     }
-    rebase<REF>(r, block_max256(r.M, red), REF ? block_max256(r.Mq, red) : kLowest, it, iq);
+    rebase<REF>(r, block_max256(r.M, red), REF ? block_max256(r.Mq, red) : kLowest, kz, kq);
     r.s = block_sum256(r.s, red);
     r.t = block_sum256(r.t, red);
     if (REF) {
@@ -203,22 +209,23 @@ __global__ void __launch_bounds__(kRowThreads) row_stats_kernel(RowArgs a, int S
     }
 }
 
-// What the gradient of a row needs: dz = scale e^x (c_ent x + c_kl (x - y) + k0) with x, y relative to M,
-// Mq, plus at the token `at`.
+// What the gradient of a row needs: dz = 2^x (A x + C (x - y) + B), x and y relative to M and Mq, plus `at`
+// at the token.
 struct RowCoef {
-    float M, Mq, scale, k0, at, dead;
+    float M, Mq, A, B, C, at, dead, pad;
 };
 
 // The row's numbers from its sums, in 64 bits: differences of logits and their logarithms decide on which
 // side of the clipping border a ratio falls.
 __device__ __forceinline__ RowCoef row_numbers(const RowArgs &a, long i, const RowStats &r, float &logp, float &entropy,
                                                double (&terms)[4]) {
-    RowCoef c = {r.M, r.Mq, 0.f, 0.f, 0.f, 1.f};
+    constexpr double ln2 = 0.693147180559945309417;
+    RowCoef c = {r.M, r.Mq, 0.f, 0.f, 0.f, 0.f, 1.f, 0.f};
     logp = entropy = 0.f;
     terms[0] = terms[1] = terms[2] = terms[3] = 0.0;
     if (!row_counts(a, i) || r.s == 0.f || (a.q != nullptr && r.sq == 0.f)) return c;
-    const double lns = log((double)r.s), lp = ((double)r.za - (double)r.M) * a.it - lns;
-    const double H = lns - (double)r.t / (double)r.s;
+    const double s = (double)r.s, lns = log(s), lp = ((double)r.za - (double)r.M) * a.it - lns;
+    const double H = lns - ln2 * (double)r.t / s;
     logp = (float)lp;
     entropy = (float)H;
     c.dead = 0.f;
@@ -232,7 +239,7 @@ __device__ __forceinline__ RowCoef row_numbers(const RowArgs &a, long i, const R
     double by_lp = cut ? 0.0 : -plain, kl = 0.0, k0 = a.c_ent * (H - lns);
     if (a.q != nullptr) {
         const double lnq = log((double)r.sq);
-        kl = (double)r.k / (double)r.s - lns + lnq;
+        kl = ln2 * (double)r.k / s - lns + lnq;
         if (a.c_kl != 0.0) k0 += a.c_kl * (lnq - lns - kl);
     } else if (a.ref_logp != nullptr) {
         const double d = (double)a.ref_logp[i] - lp, ed = exp(d);
@@ -240,8 +247,9 @@ __device__ __forceinline__ RowCoef row_numbers(const RowArgs &a, long i, const R
         if (a.c_kl != 0.0) by_lp += a.c_kl * (1.0 - ed);
     }
     const double scale = w * a.it;
-    c.scale = (float)(scale / (double)r.s);
-    c.k0 = (float)(k0 - by_lp);
+    c.A = (float)(scale / s * ln2 * a.c_ent);
+    c.B = (float)(scale / s * (k0 - by_lp));
+    c.C = (float)(scale / s * ln2 * a.c_kl);
     c.at = (float)(scale * by_lp);
     terms[0] = w * pol;
     terms[1] = w * kl;
@@ -255,12 +263,11 @@ template <bool REF>
 __device__ __forceinline__ RowStats join_parts(const RowArgs &a, long i, int S, int per, int chunk) {
     const RowStats *part = a.part + i * S;
     RowStats r = part[0];
-    const float it = (float)a.it, iq = (float)a.iq;
     for (int p = 1; p < S; ++p) {
         RowStats o = part[p];
         const float M = fmaxf(r.M, o.M), Mq = fmaxf(r.Mq, o.Mq);
-        rebase<REF>(r, M, Mq, it, iq);
-        rebase<REF>(o, M, Mq, it, iq);
+        rebase<REF>(r, M, Mq, a.kz, a.kq);
+        rebase<REF>(o, M, Mq, a.kz, a.kq);
         r.s += o.s;
         r.t += o.t;
         if (REF) {
@@ -290,26 +297,25 @@ __global__ void __launch_bounds__(64) row_finish_kernel(RowArgs a, RowCoef *coef
     for (int k = 0; k < 4; ++k) a.row_terms[i * 4 + k] = terms[k];
 }
 
-// The gradient of one chunk: chunk c of the row.
+// The gradient of one chunk, without the token's own term.
 template <DType T, bool REF>
-__device__ __forceinline__ void grad_chunk(const RowCoef &r, const uint4 &zc, const uint4 &qc, float it, float iq,
-                                           float c_kl, float c_ent, int first, int at, float *g) {
+__device__ __forceinline__ void grad_chunk(const RowCoef &r, const uint4 &zc, const uint4 &qc, float kz, float kq, float *g) {
     constexpr int N = Chunk<T>::N;
     float z[N], q[N];
     unpack_frag<T>(zc, z);
     if (REF) unpack_frag<T>(qc, q);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float x = (z[k] - r.M) * it, e = __builtin_amdgcn_exp2f(x * kLog2e);
-        const float xc = fmaxf(x, -1e4f);
-        float in = c_ent * xc + r.k0;
-        if (REF) in += c_kl * (xc - (q[k] - r.Mq) * iq);
-        g[k] = (REF && e == 0.f) ? 0.f : r.scale * e * in;
+        const float x = (z[k] - r.M) * kz, e = __builtin_amdgcn_exp2f(x);
+        float in = r.A * x + r.B;
+        if (REF) in += r.C * (x - (q[k] - r.Mq) * kq);
+        g[k] = mul0(e, in);
     }
-    if (at >= first && at < first + N) {
+}
+template <DType T>
+__device__ __forceinline__ void add_token(float *g, int k0, float v) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) g[k] += k == at - first ? r.at : 0.f;
-    }
+    for (int k = 0; k < Chunk<T>::N; ++k) g[k] += k == k0 ? v : 0.f;
 }
 
 template <DType T, bool REF>
@@ -324,7 +330,6 @@ __global__ void __launch_bounds__(kRowThreads) row_grad_kernel(RowArgs a, const 
     const int c1 = min(nch, (p + 1) * per);
     const RowCoef r = coef[i];
     const int at = a.tok[i];
-    const float it = (float)a.it, iq = (float)a.iq, c_kl = (float)a.c_kl, c_ent = (float)a.c_ent;
     for (int c = p * per + threadIdx.x; c < c1; c += kRowThreads) {
         float g[Chunk<T>::N];
         if (r.dead != 0.f) {
@@ -332,10 +337,184 @@ __global__ void __launch_bounds__(kRowThreads) row_grad_kernel(RowArgs a, const 
             for (int k = 0; k < Chunk<T>::N; ++k) g[k] = 0.f;
         } else {
             const uint4 zc = Chunk<T>::load(z, c, a.V), qc = REF ? Chunk<T>::load(q, c, a.V) : zc;
-            grad_chunk<T, REF>(r, zc, qc, it, iq, c_kl, c_ent, c * Chunk<T>::N, at, g);
+            grad_chunk<T, REF>(r, zc, qc, a.kz, a.kq, g);
+            if (c == at / Chunk<T>::N) add_token<T>(g, at % Chunk<T>::N, r.at);
         }
         Chunk<T>::store(dz, c, a.V, g);
     }
+}
+
+// One workgroup a row, the row in registers: read once, its maximum, its sums, its numbers, its gradient
+// written.  Thread t holds chunks t, t + NT, ...; NT NC of them at most, and with BIG those past that are
+// read twice, once for the sums with running maxima and once (from the last-level cache) for the gradient.
+template <DType T, bool REF, int NT, int NC, bool BIG>
+__global__ void __launch_bounds__(NT) row_fused_kernel(RowArgs a) {
+    typedef typename St<T>::type E;
+    constexpr int N = Chunk<T>::N, NW = NT / 64;
+    __shared__ float redm[2][NW], reds[4][NW];
+    __shared__ RowCoef coef;
+    const long i = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int nfull = a.V / N, nch = (a.V + N - 1) / N;
+    E *dz = (E *)a.dz + i * a.lddz;
+    if (!row_counts(a, i)) {
+        if (a.dz != nullptr) {
+            const float zero[N] = {};
+            for (int c = tid; c < nch; c += NT) Chunk<T>::store(dz, c, a.V, zero);
+        }
+        if (tid == 0) {
+            if (a.logp != nullptr) a.logp[i] = 0.f;
+            if (a.entropy != nullptr) a.entropy[i] = 0.f;
+            if (a.policy)
+                for (int k = 0; k < 4; ++k) a.row_terms[i * 4 + k] = 0.0;
+        }
+        return;
+    }
+    const E *z = (const E *)a.z + i * a.ldz;
+    const E *q = REF ? (const E *)a.q + i * a.ldq : nullptr;
+    const float kz = a.kz, kq = a.kq;
+    const uint4 none = uint4{Chunk<T>::kNegInf, Chunk<T>::kNegInf, Chunk<T>::kNegInf, Chunk<T>::kNegInf};
+    uint4 zr[NC], qr[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {  // all loads in flight; past the row the last whole chunk again, replaced below
+        zr[c] = none;
+        if (REF) qr[c] = none;
+        if (c * NT < nfull) {
+            const size_t at = (size_t)min(tid + c * NT, nfull - 1) * N;
+            zr[c] = ld16(z + at);
+            if (REF) qr[c] = ld16(q + at);
+        }
+    }
+    const int at = a.tok[i];
+    const float za = St<T>::load(z, at);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        if (c * NT < nch && (c + 1) * NT > nfull) {  // where the row ends
+            const int cc = tid + c * NT;
+            if (cc >= nfull) {
+                zr[c] = none;
+                if (REF) qr[c] = none;
+                if (cc < nch) {
+                    zr[c] = Chunk<T>::load(z, cc, a.V);
+                    if (REF) qr[c] = Chunk<T>::load(q, cc, a.V);
+                }
+            }
+        }
+    RowStats r = {kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, za, 0.f};
+    if (BIG) {
+        constexpr int U = REF ? 2 : 4;
+        for (int c = NC * NT + tid; c < nch; c += NT * U) {
+            uint4 zc[U], qc[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int cc = c + u * NT < nch ? c + u * NT : c;
+                zc[u] = Chunk<T>::load(z, cc, a.V);
+                if (REF) qc[u] = Chunk<T>::load(q, cc, a.V);
+            }
+            float M = r.M, Mq = r.Mq;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                M = fmaxf(M, chunk_max<T>(zc[u]));
+                if (REF) Mq = fmaxf(Mq, chunk_max<T>(qc[u]));
+            }
+            rebase<REF>(r, M, Mq, kz, kq);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c + u * NT < nch) add_chunk<T, REF>(r, zc[u], REF ? qc[u] : zc[u], kz, kq);
+        }
+    }
+    float M = r.M, Mq = r.Mq;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        if (c * NT < nch) {
+            M = fmaxf(M, chunk_max<T>(zr[c]));
+            if (REF) Mq = fmaxf(Mq, chunk_max<T>(qr[c]));
+        }
+    M = wave_max(M);
+    if (REF) Mq = wave_max(Mq);
+    if (NW > 1) {
+        if (lane == 0) {
+            redm[0][w] = M;
+            if (REF) redm[1][w] = Mq;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            M = fmaxf(M, redm[0][k]);
+            if (REF) Mq = fmaxf(Mq, redm[1][k]);
+        }
+    }
+    if (BIG) {
+        rebase<REF>(r, M, Mq, kz, kq);
+    } else {
+        r.M = M;
+        r.Mq = Mq;
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        if (c * NT < nch) add_chunk<T, REF>(r, zr[c], REF ? qr[c] : zr[c], kz, kq);
+    r.s = wave_sum(r.s);
+    r.t = wave_sum(r.t);
+    if (REF) {
+        r.k = wave_sum(r.k);
+        r.sq = wave_sum(r.sq);
+    }
+    if (NW > 1) {
+        if (lane == 0) {
+            reds[0][w] = r.s;
+            reds[1][w] = r.t;
+            if (REF) {
+                reds[2][w] = r.k;
+                reds[3][w] = r.sq;
+            }
+        }
+        __syncthreads();
+    }
+    if (w == 0) {
+        if (NW > 1) {
+            r.s = wave_sum(lane < NW ? reds[0][lane & (NW - 1)] : 0.f);
+            r.t = wave_sum(lane < NW ? reds[1][lane & (NW - 1)] : 0.f);
+            if (REF) {
+                r.k = wave_sum(lane < NW ? reds[2][lane & (NW - 1)] : 0.f);
+                r.sq = wave_sum(lane < NW ? reds[3][lane & (NW - 1)] : 0.f);
+            }
+        }
+        float logp, entropy;
+        double terms[4];
+        const RowCoef c = row_numbers(a, i, r, logp, entropy, terms);
+        if (lane == 0) {
+            coef = c;
+            if (a.logp != nullptr) a.logp[i] = logp;
+            if (a.entropy != nullptr) a.entropy[i] = entropy;
+            if (a.policy)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a.row_terms[i * 4 + k] = terms[k];
+        }
+    }
+    if (a.dz == nullptr) return;
+    __syncthreads();
+    const RowCoef rc = coef;
+    const bool dead = rc.dead != 0.f, kl = REF && rc.C != 0.f;
+    auto put = [&](int c, const uint4 &zc, const uint4 &qc) {  // chunk c of the row
+        float g[N];
+        if (dead) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) g[k] = 0.f;
+        } else {
+            if (kl)
+                grad_chunk<T, REF>(rc, zc, qc, kz, kq, g);
+            else
+                grad_chunk<T, false>(rc, zc, zc, kz, kq, g);
+            if (c == at / N) add_token<T>(g, at % N, rc.at);
+        }
+        Chunk<T>::store(dz, c, a.V, g);
+    };
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+        if (tid + c * NT < nch) put(tid + c * NT, zr[c], REF ? qr[c] : zr[c]);
+    if (BIG)
+        for (int c = NC * NT + tid; c < nch; c += NT)
+            put(c, Chunk<T>::load(z, c, a.V), REF ? Chunk<T>::load(q, c, a.V) : none);
 }
 
 // The loss and its terms, the rows in a fixed order.
@@ -381,9 +560,35 @@ size_t rows_workspace(long N, int V, bool policy) {
     return up256((size_t)N * S * sizeof(RowStats)) + (policy ? up256((size_t)N * 32) + up256((size_t)N * sizeof(RowCoef)) : 0);
 }
 
+// Whether a row is one workgroup's (row_fused_kernel) or is split over several.
+static bool row_whole(long N, int V) { return true; }
+
+template <DType T, bool REF>
+static void launch_fused(const RowArgs &a, int nch, hipStream_t s) {
+    const unsigned n = (unsigned)a.N;
+    if (nch <= 64 * 4)
+        row_fused_kernel<T, REF, 64, 4, false><<<n, 64, 0, s>>>(a);
+    else if (nch <= 256 * 4)
+        row_fused_kernel<T, REF, 256, 4, false><<<n, 256, 0, s>>>(a);
+    else if (nch <= 256 * 8)
+        row_fused_kernel<T, REF, 256, 8, false><<<n, 256, 0, s>>>(a);
+    else if (nch <= 512 * 8)
+        row_fused_kernel<T, REF, 512, 8, false><<<n, 512, 0, s>>>(a);
+    else if (nch <= 1024 * 8)
+        row_fused_kernel<T, REF, 1024, 8, false><<<n, 1024, 0, s>>>(a);
+    else
+        row_fused_kernel<T, REF, 1024, 8, true><<<n, 1024, 0, s>>>(a);
+}
+
 template <DType T, bool REF>
 static void launch_rows_t(RowArgs a, void *workspace, hipStream_t s) {
     const int nch = (a.V + Chunk<T>::N - 1) / Chunk<T>::N;
+    if (a.N > 0 && row_whole(a.N, a.V)) {
+        a.row_terms = (double *)workspace;
+        launch_fused<T, REF>(a, nch, s);
+        if (a.policy) row_terms_kernel<<<1, 1024, 0, s>>>(a);
+        return;
+    }
     int per;
     const int S = row_parts(a.N > 0 ? a.N : 1, nch, per);
     uint8_t *w = (uint8_t *)workspace;
@@ -408,6 +613,9 @@ static void launch_rows_t(RowArgs a, void *workspace, hipStream_t s) {
 }
 
 void launch_rows(DType t, RowArgs a, void *workspace, hipStream_t s) {
+    constexpr double log2e = 1.44269504088896340736;
+    a.kz = (float)(a.it * log2e);
+    a.kq = (float)(a.iq * log2e);
     if (t == DType::BF16)
         a.q != nullptr ? launch_rows_t<DType::BF16, true>(a, workspace, s) : launch_rows_t<DType::BF16, false>(a, workspace, s);
     else
@@ -585,8 +793,11 @@ template <> struct State<8> {
 // at random so that the mean is right: v moves by 1 - b2 of itself a step, far less than half a spacing of
 // e4m3, and would stay where it is under rounding to nearest.  The step itself uses m and v before that
 // rounding.  A root that is not zero is kept from rounding to zero, which would blow the next step up.
+// Every operation rounds by itself (no fused multiply-add): near the border of a random rounding the codes
+// then are those of the same formulas in any other IEEE arithmetic of 32 bits.
 template <DType PT, bool MASTER, DType GT, int BITS>
 __global__ void __launch_bounds__(256) adamw_kernel(AdamTable tab, AdamArgs a) {
+#pragma clang fp contract(off)
     __shared__ double red[4];
     float clip = 1.f;
     if (a.norm_part != nullptr) {
@@ -646,7 +857,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamTable tab, AdamArgs a) {
         for (int k = 0; k < 4; ++k) {
             const float gk = g[u][k] * clip;
             m[k] = a.b1 * m[k] + a.one_b1 * gk;
-            v[k] = a.b2 * v[k] + a.one_b2 * (gk * gk);
+            v[k] = a.b2 * v[k] + a.one_b2 * gk * gk;
             r[k] = sqrtf(v[k]);
             p[u][k] = p[u][k] * a.decay - a.rate * m[k] / (r[k] * a.root + a.eps);
         }
