@@ -222,7 +222,7 @@ def run(s):
                                     c_kl=C_KL if case["ref"] != "none" else 0.0, c_ent=C_ENT)
             return {"terms": out.terms, "logp": out.logp, "grad": out.grad}
         s.opt.step(s.grads)
-        return _updated(s, s.opt.grad_norm)
+        return _updated(s, s.opt.grad_norm[0] if case["clip"] else None)
     if case["op"] == "logp":
         return _plain_logp(s)
     if case["op"] == "policy":
