@@ -266,8 +266,8 @@ const char *dvi_op_error(void);
 
 /*
  * Rows of logits: DEVICE [rows, vocab] of dtype, row i at logits + i * ld elements (ld >= 0, any
- * alignment of its elements; rows may overlap, as an expanded row's do; at most 2^22 rows); temperature
- * > 0 divides them.
+ * alignment of its elements; rows may overlap, as an expanded row's do; at most 2^22 rows of at most 2^28
+ * entries); temperature, from 1e-6 to 1e6, divides them.
  * tokens: DEVICE int32 [rows].  A row whose token lies outside [0, vocab) or that has no logit above
  * -inf is masked: its outputs are 0.  Logits of -inf (or the type's lowest number) are tokens of
  * probability 0.  A NaN, or +inf, among a row's logits makes its outputs NaN.

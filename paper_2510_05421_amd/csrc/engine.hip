@@ -1375,7 +1375,9 @@ static bool rows_apart(const void *p, int64_t pld, const void *q, int64_t qld, i
     return off >= width && off <= row - width;
 }
 
-// The largest number of rows (a launch's threads are counted in 32 bits), and the widest stride.
+// The largest number of rows (a launch's threads are counted in 32 bits), the widest stride, and the largest
+// vocabulary (a row's bytes are counted in 32 bits).
+static constexpr int32_t kMaxOpVocab = 1 << 28;
 static constexpr int64_t kMaxOpRows = (int64_t)1 << 22, kMaxOpStride = (int64_t)1 << 36;
 
 static dvi_status check_rows(int64_t rows, int32_t vocab, dvi_dtype dtype, const void *logits, int64_t ld,
@@ -1384,7 +1386,8 @@ static dvi_status check_rows(int64_t rows, int32_t vocab, dvi_dtype dtype, const
     if (rows < 0) return op_fail(DVI_ERR_ARG, "rows must not be negative");
     if (rows > kMaxOpRows) return op_fail(DVI_ERR_CAPACITY, "at most %lld rows", (long long)kMaxOpRows);
     if (vocab < 1) return op_fail(DVI_ERR_ARG, "vocab must be at least 1");
-    if (!(temperature > 0.0) || !(temperature < 1e30)) return op_fail(DVI_ERR_ARG, "temperature must be > 0 and finite");
+    if (vocab > kMaxOpVocab) return op_fail(DVI_ERR_CAPACITY, "at most %d entries", kMaxOpVocab);
+    if (!(temperature >= 1e-6 && temperature <= 1e6)) return op_fail(DVI_ERR_ARG, "temperature must be from 1e-6 to 1e6");
     if (rows == 0) return DVI_OK;
     if (logits == nullptr || tokens == nullptr) return op_fail(DVI_ERR_ARG, "logits and tokens must be given");
     if (ld < 0 || ld > kMaxOpStride) return op_fail(DVI_ERR_ARG, "row strides from 0 to 2^36");
@@ -1393,7 +1396,7 @@ static dvi_status check_rows(int64_t rows, int32_t vocab, dvi_dtype dtype, const
 }
 
 extern "C" size_t dvi_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab) {
-    return rows < 0 || rows > kMaxOpRows || vocab < 1 ? 0 : rows_workspace(rows, vocab, false);
+    return rows < 0 || rows > kMaxOpRows || vocab < 1 || vocab > kMaxOpVocab ? 0 : rows_workspace(rows, vocab, false);
 }
 
 extern "C" dvi_status dvi_token_logprobs(const dvi_logprob_args *g, void *workspace, size_t ws_bytes, void *hip_stream) {
@@ -1418,7 +1421,7 @@ extern "C" dvi_status dvi_token_logprobs(const dvi_logprob_args *g, void *worksp
 }
 
 extern "C" size_t dvi_policy_loss_workspace_bytes(int64_t rows, int32_t vocab) {
-    return rows < 0 || rows > kMaxOpRows || vocab < 1 ? 0 : rows_workspace(rows, vocab, true);
+    return rows < 0 || rows > kMaxOpRows || vocab < 1 || vocab > kMaxOpVocab ? 0 : rows_workspace(rows, vocab, true);
 }
 
 extern "C" dvi_status dvi_policy_loss(const dvi_policy_args *g, void *workspace, size_t ws_bytes, void *hip_stream) {
@@ -1434,8 +1437,8 @@ extern "C" dvi_status dvi_policy_loss(const dvi_policy_args *g, void *workspace,
     if (g->c_kl != 0.0 && !g->ref_logits && !g->ref_logp) return op_fail(DVI_ERR_ARG, "c_kl needs ref_logits or ref_logp");
     const size_t es = op_size(g->dtype);
     if (g->ref_logits) {
-        if (!(g->ref_temperature > 0.0) || !(g->ref_temperature < 1e30))
-            return op_fail(DVI_ERR_ARG, "ref_temperature must be > 0 and finite");
+        if (!(g->ref_temperature >= 1e-6 && g->ref_temperature <= 1e6))
+            return op_fail(DVI_ERR_ARG, "ref_temperature must be from 1e-6 to 1e6");
         if (g->ref_ld < 0 || g->ref_ld > kMaxOpStride) return op_fail(DVI_ERR_ARG, "row strides from 0 to 2^36");
         if ((uintptr_t)g->ref_logits % es) return op_fail(DVI_ERR_ARG, "ref_logits are not aligned to their type");
     }

@@ -10,9 +10,10 @@ namespace dvi {
 
 // What the kernels keep of a part of a row: with x = (z - M) log2(e) / T and y = (ref - Mq) log2(e) / Tr,
 // s = sum 2^x, t = sum 2^x x, k = sum 2^x (x - y), sq = sum 2^y; za: the token's logit, where the part
-// holds it.  M and Mq start at the lowest finite number, so s == 0 says that there is no logit above -inf.
+// holds it; top: 1 where s leaves the largest logit itself out.  M and Mq start at the lowest finite number,
+// so s == 0 (and top == 0) says that there is no logit above -inf.
 struct RowStats {
-    float M, s, t, k, Mq, sq, za, pad;
+    float M, s, t, k, Mq, sq, za, top;
 };
 
 struct RowArgs {

@@ -5,6 +5,9 @@
 // few times as the caches allow, 16 bytes a lane, and keeps everything else in registers.
 #include "learn.h"
 
+#include <algorithm>
+#include <type_traits>
+
 #include "device.h"
 
 namespace dvi {
@@ -25,81 +28,152 @@ __device__ __forceinline__ uint4 ld16(const void *p) {
     const v4u v = *(const v4u_any *)p;
     return uint4{v.x, v.y, v.z, v.w};
 }
+// Read once, or written and not read again: past the caches (rows of 32000 in bf16 read at 6.1 TB/s so, at
+// 5.3 with ordinary loads; the loss with its gradient, 4096 rows, 112 -> 108 us with such stores).
+__device__ __forceinline__ uint4 ld16_once(const void *p) {
+    const v4u v = __builtin_nontemporal_load((const v4u_any *)p);
+    return uint4{v.x, v.y, v.z, v.w};
+}
 __device__ __forceinline__ void st16(void *p, const uint4 &r) { *(v4u_any *)p = v4u{r.x, r.y, r.z, r.w}; }
-
+__device__ __forceinline__ void st16_once(void *p, const uint4 &r) {
+    __builtin_nontemporal_store(v4u{r.x, r.y, r.z, r.w}, (v4u_any *)p);
+}
 template <DType T> struct Chunk {
     typedef typename St<T>::type E;
     static constexpr int N = 16 / (int)sizeof(E);
     static constexpr uint32_t kNegInf = T == DType::BF16 ? 0xff80ff80u : 0xff800000u;
-    static __device__ __forceinline__ uint4 load(const E *row, int c, int V) {
-        uint4 r;
-        if ((c + 1) * N <= V) {
-            r = ld16(row + (size_t)c * N);
-        } else {
-            E e[N];
-#pragma unroll
-            for (int k = 0; k < N; ++k) e[k] = c * N + k < V ? row[(size_t)c * N + k] : (E)0;
-            __builtin_memcpy(&r, e, 16);
-            uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (c * N + k >= V) {
-                    if (T == DType::BF16)
-                        w[k / 2] = (k & 1) ? (w[k / 2] & 0xffffu) | 0xff800000u : (w[k / 2] & 0xffff0000u) | 0xff80u;
-                    else
-                        w[k] = kNegInf;
+
+    // The last V % N elements (V % N > 0) and -inf behind them: the row's last 16 bytes moved down, or one by
+    // one where the row is shorter than that.  V is the same for the whole launch.
+    static __device__ __forceinline__ uint4 tail(const E *row, int V) {
+        const int n = V % N;
+        uint32_t w[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+        if (V >= N) {
+            const uint4 t = ld16((const uint8_t *)row + (uint32_t)(V - N) * (uint32_t)sizeof(E));
+            w[0] = t.x, w[1] = t.y, w[2] = t.z, w[3] = t.w;
+            int drop = N - n;
+            if (T == DType::BF16) {
+                if (drop & 1) {
+                    w[0] = __builtin_amdgcn_alignbyte(w[1], w[0], 2);
+                    w[1] = __builtin_amdgcn_alignbyte(w[2], w[1], 2);
+                    w[2] = __builtin_amdgcn_alignbyte(w[3], w[2], 2);
+                    w[3] = __builtin_amdgcn_alignbyte(kNegInf, w[3], 2);
                 }
-            r = uint4{w[0], w[1], w[2], w[3]};
-        }
-        return r;
-    }
-    static __device__ __forceinline__ void store(E *row, int c, int V, const float *v) {
-        const uint4 r = pack_frag_cvt<T>(v);
-        if ((c + 1) * N <= V) {
-            st16(row + (size_t)c * N, r);
-        } else {
-            E e[N];
-            __builtin_memcpy(e, &r, 16);
+                drop >>= 1;
+            }
+            for (; drop > 0; --drop) {
+                w[0] = w[1];
+                w[1] = w[2];
+                w[2] = w[3];
+                w[3] = kNegInf;
+            }
+        } else if (T == DType::BF16) {
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (c * N + k < V) row[(size_t)c * N + k] = e[k];
-        }
-    }
-};
-template <> struct Chunk<DType::F32> {
-    typedef float E;
-    static constexpr int N = 4;
-    static constexpr uint32_t kNegInf = 0xff800000u;
-    static __device__ __forceinline__ uint4 load(const float *row, int c, int V) {
-        uint4 r;
-        if ((c + 1) * 4 <= V) {
-            r = ld16(row + (size_t)c * 4);
-        } else {
-            float e[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) e[k] = c * 4 + k < V ? row[(size_t)c * 4 + k] : -INFINITY;
-            __builtin_memcpy(&r, e, 16);
-        }
-        return r;
-    }
-    static __device__ __forceinline__ void store(float *row, int c, int V, const float *v) {
-        if ((c + 1) * 4 <= V) {
-            st16(row + (size_t)c * 4, pack_frag_cvt<DType::F32>(v));
+            for (int k = 0; k < 7; ++k)
+                if (k < n) {
+                    const uint32_t b = ((const uint16_t *)row)[k];
+                    w[k / 2] = (k & 1) ? (w[k / 2] & 0xffffu) | (b << 16) : (w[k / 2] & 0xffff0000u) | b;
+                }
         } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c * 4 + k < V) row[(size_t)c * 4 + k] = v[k];
+            for (int k = 0; k < 3; ++k)
+                if (k < n) w[k] = ((const uint32_t *)row)[k];
         }
+        return uint4{w[0], w[1], w[2], w[3]};
+    }
+    static __device__ __forceinline__ void store_tail(E *row, int V, const uint4 &r) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+        const int first = V / N * N;
+#pragma unroll
+        for (int k = 0; k < N - 1; ++k)
+            if (k < V % N) {
+                if (T == DType::BF16)
+                    ((uint16_t *)row)[first + k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
+                else
+                    ((uint32_t *)row)[first + k] = w[k];
+            }
+    }
+    // all but the first element
+    static __device__ __forceinline__ void store_first(uint16_t *row, const uint4 &r) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 1; k < 8; ++k) row[k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
     }
 };
 
 constexpr float kLowest = -3.402823466e38f;
 
-// Whether row i takes part: a weight other than 0 and a token of the vocabulary.
-__device__ __forceinline__ bool row_counts(const RowArgs &a, long i) {
-    const uint32_t t = (uint32_t)a.tok[i];
-    return t < (uint32_t)a.V && !(a.weights != nullptr && a.weights[i] == 0.f);
+// What is one number a row, read at the start (beside the logits on their way); and whether the row takes
+// part: a weight other than 0 and a token of the vocabulary.
+struct RowIn {
+    int tok;
+    float w, adv, old, ref;
+    bool on, counts;
+};
+__device__ __forceinline__ RowIn row_in(const RowArgs &a, long i) {
+    RowIn r = {a.tok[i], 1.f, 0.f, 0.f, 0.f, true, false};
+    if (a.policy) {
+        r.w = a.weights != nullptr ? a.weights[i] : a.w0;
+        r.adv = a.adv[i];
+        if (a.old != nullptr) {
+            r.old = a.old[i];
+            r.on = a.on_policy != nullptr && a.on_policy[i] != 0;
+        }
+        if (a.ref_logp != nullptr) r.ref = a.ref_logp[i];
+    }
+    r.counts = (uint32_t)r.tok < (uint32_t)a.V && r.w != 0.f;
+    return r;
 }
+
+// Where a row lies.  A bf16 row that starts between two 32-bit words counts from one element earlier
+// (lead = 1), so that its chunks start on words: 16 bytes at an odd element load at three quarters of the
+// rate (1024 rows of 65521 entries 73 -> 61 us), at any word at the full one, and stores at either.  Chunk 0
+// then holds -inf in front.
+template <DType T> struct Row {
+    typedef typename St<T>::type E;
+    const E *z, *q;  // less the lead
+    E *dz;
+    int lead, V, at, nfull, nch;  // entries and token with the lead; whole chunks, all chunks
+    __device__ __forceinline__ Row(const RowArgs &a, long i, int tok, bool ref) {
+        constexpr int N = Chunk<T>::N;
+        z = (const E *)a.z + i * a.ldz;
+        lead = T == DType::BF16 && a.V >= N ? (int)(((uintptr_t)z >> 1) & 1) : 0;
+        z -= lead;
+        q = ref ? (const E *)a.q + i * a.ldq - lead : nullptr;
+        dz = (E *)a.dz + i * a.lddz - lead;
+        V = a.V + lead;
+        at = tok + lead;
+        nfull = V / N;
+        nch = (V + N - 1) / N;
+    }
+    // Whole chunk c as it lies in memory; chunk 0 of a row with a lead needs first() then.
+    template <bool ONCE>
+    __device__ __forceinline__ uint4 load(const E *row, int c) const {
+        const uint32_t off = T == DType::BF16 ? max((uint32_t)c * 16u, (uint32_t)lead * 2u) : (uint32_t)c * 16u;
+        return ONCE ? ld16_once((const uint8_t *)row + off) : ld16((const uint8_t *)row + off);
+    }
+    __device__ __forceinline__ void first(uint4 &r) const {
+        r.w = __builtin_amdgcn_alignbyte(r.w, r.z, 2);
+        r.z = __builtin_amdgcn_alignbyte(r.z, r.y, 2);
+        r.y = __builtin_amdgcn_alignbyte(r.y, r.x, 2);
+        r.x = __builtin_amdgcn_alignbyte(r.x, 0xff80ff80u, 2);
+    }
+    // Any chunk of the row (slow where the row begins or ends in it).
+    __device__ __forceinline__ uint4 any(const E *row, int c) const {
+        if (c >= nfull) return Chunk<T>::tail(row, V);
+        uint4 r = load<false>(row, c);
+        if (T == DType::BF16 && lead && c == 0) first(r);
+        return r;
+    }
+    __device__ __forceinline__ void store(int c, const uint4 &r) const {
+        if (c >= nfull)
+            Chunk<T>::store_tail(dz, V, r);
+        else if (T == DType::BF16 && lead && c == 0)
+            Chunk<T>::store_first((uint16_t *)dz, r);
+        else
+            st16_once((uint8_t *)dz + (uint32_t)c * 16u, r);
+    }
+};
 
 // a * b with 0 * anything == 0: a probability of 0 takes no part, whatever it is multiplied with.
 // (The compiler has to know the instruction: it keeps a product that follows an exponential of its wave at
@@ -107,23 +181,39 @@ __device__ __forceinline__ bool row_counts(const RowArgs &a, long i) {
 __device__ float fmul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
 __device__ __forceinline__ float mul0(float a, float b) { return fmul_legacy(a, b); }
 
-// The sums of one more chunk.  x = (z - M) log2(e) / T and y of the reference likewise (kz, kq: log2(e) over
-// the temperature); the terms are 2^x, 2^x x and, for the KL divergence, 2^x (x - y): differences of logits
-// that are already relative to their maxima, so nothing large cancels.  A -inf (2^x == 0) adds nothing even
-// where x or y is infinite; a NaN makes the sums NaN.
+// x = z k - b is a logit in base-2 units relative to its row's maximum M: k = log2(e) / T, b = M k as rounded,
+// so that every exponential of a row is off by the same factor 2^(M k - b), which the row's numbers take out
+// again.  That factor grows with |M k|.  From 2^31 on (rows that are masked with large negative numbers as
+// a whole), logits that differ at all differ by more than any exponential can show: a power of two near k, by
+// which M k is exact, serves as well, and one 2^60 times smaller where M k would leave fp32's range.
+struct Scale {
+    float k, b;
+    __device__ __forceinline__ float of(float z) const { return fmaf(z, k, -b); }
+};
+__device__ __forceinline__ Scale scale_of(float M, float k) {
+#pragma clang fp contract(off)  // b is the rounded product wherever it goes
+    const float two = __uint_as_float(__float_as_uint(k) & 0x7f800000u), p = fabsf(M * k);
+    k = p < 0x1p31f ? k : p < 0x1p100f ? two : two * 0x1p-60f;
+    return {k, M * k};
+}
+
+// The sums of one more chunk, x of the logits and y of the reference's: s = sum 2^x, t = sum 2^x x and, for the
+// KL divergence, k = sum 2^x (x - y): differences of logits that are already relative to their maxima, so
+// nothing large cancels.  A -inf (2^x == 0) adds nothing even where x or y is infinite; a NaN makes the
+// sums NaN.
 template <DType T, bool REF>
-__device__ __forceinline__ void add_chunk(RowStats &r, const uint4 &zc, const uint4 &qc, float kz, float kq) {
+__device__ __forceinline__ void add_chunk(RowStats &r, const uint4 &zc, const uint4 &qc, Scale sz, Scale sq) {
     constexpr int N = Chunk<T>::N;
     float z[N], q[N];
     unpack_frag<T>(zc, z);
     if (REF) unpack_frag<T>(qc, q);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float x = (z[k] - r.M) * kz, e = __builtin_amdgcn_exp2f(x);
+        const float x = sz.of(z[k]), e = __builtin_amdgcn_exp2f(x);
         r.s += e;
         r.t += mul0(e, x);
         if (REF) {
-            const float y = (q[k] - r.Mq) * kq;
+            const float y = sq.of(q[k]);
             r.sq += __builtin_amdgcn_exp2f(y);
             r.k += mul0(e, x - y);
         }
@@ -133,10 +223,10 @@ __device__ __forceinline__ void add_chunk(RowStats &r, const uint4 &zc, const ui
 // Sums relative to new maxima M, Mq (at least the old ones).
 template <bool REF>
 __device__ __forceinline__ void rebase(RowStats &r, float M, float Mq, float kz, float kq) {
-    const float dx = (r.M - M) * kz, f = __builtin_amdgcn_exp2f(dx);
+    const float dx = scale_of(r.M, kz).b - scale_of(M, kz).b, f = __builtin_amdgcn_exp2f(dx);
     if (REF) {
         // a reference masked by the lowest number: dy is as large as that, and counts only where f s does
-        const float dy = (r.Mq - Mq) * kq;
+        const float dy = scale_of(r.Mq, kq).b - scale_of(Mq, kq).b;
         r.k = mul0(f, r.k + mul0(r.s, dx - dy));
         r.sq *= __builtin_amdgcn_exp2f(dy);
         r.Mq = Mq;
@@ -157,97 +247,111 @@ __device__ __forceinline__ float chunk_max(const uint4 &c) {
     return m;
 }
 
-constexpr int kRowThreads = 256;
-constexpr int kRowUnroll = 4;  // chunks that a thread has in flight
-
-// Stats of part blockIdx.x % S of row blockIdx.x / S: one pass with running maxima, four chunks a thread
-// between two looks at the maximum, then the workgroup's threads in a fixed order.
-template <DType T, bool REF>
-__global__ void __launch_bounds__(kRowThreads) row_stats_kernel(RowArgs a, int S, int per) {
-    typedef typename St<T>::type E;
-    __shared__ float red[4];
-    const long i = blockIdx.x / S;
-    const int p = (int)(blockIdx.x - i * S);
-    if (!row_counts(a, i)) return;
-    const E *z = (const E *)a.z + i * a.ldz;
-    const E *q = REF ? (const E *)a.q + i * a.ldq : nullptr;
-    const int nch = (a.V + Chunk<T>::N - 1) / Chunk<T>::N;
-    const int c1 = min(nch, (p + 1) * per);
-    const float kz = a.kz, kq = a.kq;
-    RowStats r = {kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, 0.f, 0.f};
-    for (int c = p * per + threadIdx.x; c < c1; c += kRowThreads * kRowUnroll) {
-        uint4 zc[kRowUnroll], qc[kRowUnroll];
+// The sums of U more chunks, their maxima first; chunk u counts where used[u].
+template <DType T, bool REF, int U>
+__device__ __forceinline__ void add_chunks(RowStats &r, const uint4 *zc, const uint4 *qc, const bool *used, float kz, float kq) {
+    float M = r.M, Mq = r.Mq;
 #pragma unroll
-        for (int u = 0; u < kRowUnroll; ++u) {
-            // past the part: the first chunk again, which is not added
-            const int cc = c + u * kRowThreads < c1 ? c + u * kRowThreads : c;
-            zc[u] = Chunk<T>::load(z, cc, a.V);
-            if (REF) qc[u] = Chunk<T>::load(q, cc, a.V);
-        }
-        float M = r.M, Mq = r.Mq;
+    for (int u = 0; u < U; ++u) {  // a thread's maximum is one of its own chunks'
+        M = fmaxf(M, used[u] ? chunk_max<T>(zc[u]) : kLowest);
+        if (REF) Mq = fmaxf(Mq, used[u] ? chunk_max<T>(qc[u]) : kLowest);
+    }
+    rebase<REF>(r, M, Mq, kz, kq);
+    const Scale sz = scale_of(M, kz), sq = scale_of(Mq, kq);
 #pragma unroll
-        for (int u = 0; u < kRowUnroll; ++u) {
-            M = fmaxf(M, chunk_max<T>(zc[u]));
-            if (REF) Mq = fmaxf(Mq, chunk_max<T>(qc[u]));
-        }
-        rebase<REF>(r, M, Mq, kz, kq);
-#pragma unroll
-        for (int u = 0; u < kRowUnroll; ++u)
-            if (c + u * kRowThreads < c1) add_chunk<T, REF>(r, zc[u], REF ? qc[u] : zc[u], kz, kq);
-    }
-    rebase<REF>(r, block_max256(r.M, red), REF ? block_max256(r.Mq, red) : kLowest, kz, kq);
-    r.s = block_sum256(r.s, red);
-    r.t = block_sum256(r.t, red);
-    if (REF) {
-        r.k = block_sum256(r.k, red);
-        r.sq = block_sum256(r.sq, red);
-    }
-    if (threadIdx.x == 0) {
-        const int at = a.tok[i];
-        if (at / Chunk<T>::N >= p * per && at / Chunk<T>::N < c1) r.za = St<T>::load(z, at);
-        a.part[i * S + p] = r;
-    }
+    for (int u = 0; u < U; ++u)
+        if (used[u]) add_chunk<T, REF>(r, zc[u], REF ? qc[u] : zc[u], sz, sq);
 }
 
-// What the gradient of a row needs: dz = 2^x (A x + C (x - y) + B), x and y relative to M and Mq, plus `at`
-// at the token.
+// What the gradient of a row needs: dz = 2^x (A x - C y + B), plus `at` at the token.
 struct RowCoef {
-    float M, Mq, A, B, C, at, dead, pad;
+    Scale z, q;
+    float A, B, C, at, dead, pad;
 };
+
+// exp and log of a row's numbers in 64 bits, by a Taylor and an atanh series: accurate to a few 1e-15, and short
+// enough that the rows the waves hold stay in their registers beside them.
+__device__ __forceinline__ double exp64(double x) {
+    x = x < -800.0 ? -800.0 : x > 800.0 ? 800.0 : x;  // a NaN stays one
+    const double k = rint(x * 1.4426950408889634074);
+    const double r = fma(k, -1.9082149292705877e-10, fma(k, -0.69314718036912381649, x));
+    double p = 1.0 / 39916800.0;
+    p = fma(p, r, 1.0 / 3628800.0);
+    p = fma(p, r, 1.0 / 362880.0);
+    p = fma(p, r, 1.0 / 40320.0);
+    p = fma(p, r, 1.0 / 5040.0);
+    p = fma(p, r, 1.0 / 720.0);
+    p = fma(p, r, 1.0 / 120.0);
+    p = fma(p, r, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    return ldexp(p, (int)k);
+}
+__device__ __forceinline__ double log64(double s) {  // s > 0 and normal
+    int k;
+    double m = frexp(s, &k);  // [0.5, 1)
+    if (m < 0.70710678118654752) {
+        m *= 2.0;
+        --k;
+    }
+    const double t = (m - 1.0) / (m + 1.0), t2 = t * t;
+    double p = 1.0 / 17.0;
+    p = fma(p, t2, 1.0 / 15.0);
+    p = fma(p, t2, 1.0 / 13.0);
+    p = fma(p, t2, 1.0 / 11.0);
+    p = fma(p, t2, 1.0 / 9.0);
+    p = fma(p, t2, 1.0 / 7.0);
+    p = fma(p, t2, 1.0 / 5.0);
+    p = fma(p, t2, 1.0 / 3.0);
+    p = fma(p, t2, 1.0);
+    return fma((double)k, 0.693147180559945309417, 2.0 * t * p);
+}
+
+__device__ __forceinline__ float uniform(float v) {
+    return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
+__device__ __forceinline__ RowCoef uniform(const RowCoef &c) {
+    return {{uniform(c.z.k), uniform(c.z.b)}, {uniform(c.q.k), uniform(c.q.b)}, uniform(c.A), uniform(c.B), uniform(c.C),
+            uniform(c.at), uniform(c.dead), 0.f};
+}
 
 // The row's numbers from its sums, in 64 bits: differences of logits and their logarithms decide on which
 // side of the clipping border a ratio falls.
-__device__ __forceinline__ RowCoef row_numbers(const RowArgs &a, long i, const RowStats &r, float &logp, float &entropy,
-                                               double (&terms)[4]) {
+__device__ __forceinline__ RowCoef row_numbers(const RowArgs &a, const RowIn &in, const RowStats &r, float &logp,
+                                               float &entropy, double (&terms)[4]) {
     constexpr double ln2 = 0.693147180559945309417;
-    RowCoef c = {r.M, r.Mq, 0.f, 0.f, 0.f, 0.f, 1.f, 0.f};
+    RowCoef c = {scale_of(r.M, a.kz), scale_of(r.Mq, a.kq), 0.f, 0.f, 0.f, 0.f, 1.f, 0.f};
     logp = entropy = 0.f;
     terms[0] = terms[1] = terms[2] = terms[3] = 0.0;
-    if (!row_counts(a, i) || r.s == 0.f || (a.q != nullptr && r.sq == 0.f)) return c;
-    const double s = (double)r.s, lns = log(s), lp = ((double)r.za - (double)r.M) * a.it - lns;
+    if ((r.s == 0.f && r.top == 0.f) || (a.q != nullptr && r.sq == 0.f)) return c;
+    // the factor that all of the row's exponentials share; the token's logit goes by the exact temperature
+    const double rest = ln2 * ((double)r.M * (double)c.z.k - (double)c.z.b);
+    const double s = (double)r.s + (r.top != 0.f ? (double)r.top * exp64(rest) : 0.0), lns = log64(s);
+    const double lp = ((double)r.za - (double)r.M) * a.it + rest - lns;
     const double H = lns - ln2 * (double)r.t / s;
     logp = (float)lp;
     entropy = (float)H;
     c.dead = 0.f;
     if (!a.policy) return c;
-    const double w = a.weights != nullptr ? (double)a.weights[i] : (double)a.w0, adv = (double)a.adv[i];
-    const bool on = a.old == nullptr || (a.on_policy != nullptr && a.on_policy[i] != 0);
-    const double ratio = on ? 1.0 : exp(lp - (double)a.old[i]);
+    const double w = (double)in.w, adv = (double)in.adv;
+    const double ratio = in.on ? 1.0 : exp64(lp - (double)in.old);
     const double plain = ratio * adv, held = fmin(fmax(ratio, a.lo), a.hi) * adv;
     const bool cut = held < plain;
     const double pol = cut ? -held : -plain;
     double by_lp = cut ? 0.0 : -plain, kl = 0.0, k0 = a.c_ent * (H - lns);
     if (a.q != nullptr) {
-        const double lnq = log((double)r.sq);
+        const double lnq = log64((double)r.sq);
         kl = ln2 * (double)r.k / s - lns + lnq;
         if (a.c_kl != 0.0) k0 += a.c_kl * (lnq - lns - kl);
     } else if (a.ref_logp != nullptr) {
-        const double d = (double)a.ref_logp[i] - lp, ed = exp(d);
+        const double d = (double)in.ref - lp, ed = exp64(d);
         kl = ed - d - 1.0;
         if (a.c_kl != 0.0) by_lp += a.c_kl * (1.0 - ed);
     }
     const double scale = w * a.it;
-    c.A = (float)(scale / s * ln2 * a.c_ent);
+    c.A = (float)(scale / s * ln2 * (a.q != nullptr ? a.c_ent + a.c_kl : a.c_ent));
     c.B = (float)(scale / s * (k0 - by_lp));
     c.C = (float)(scale / s * ln2 * a.c_kl);
     c.at = (float)(scale * by_lp);
@@ -258,57 +362,18 @@ __device__ __forceinline__ RowCoef row_numbers(const RowArgs &a, long i, const R
     return c;
 }
 
-// The S parts of row i as one, in order.
-template <bool REF>
-__device__ __forceinline__ RowStats join_parts(const RowArgs &a, long i, int S, int per, int chunk) {
-    const RowStats *part = a.part + i * S;
-    RowStats r = part[0];
-    for (int p = 1; p < S; ++p) {
-        RowStats o = part[p];
-        const float M = fmaxf(r.M, o.M), Mq = fmaxf(r.Mq, o.Mq);
-        rebase<REF>(r, M, Mq, a.kz, a.kq);
-        rebase<REF>(o, M, Mq, a.kz, a.kq);
-        r.s += o.s;
-        r.t += o.t;
-        if (REF) {
-            r.k += o.k;
-            r.sq += o.sq;
-        }
-    }
-    r.za = part[a.tok[i] / chunk / per].za;
-    return r;
-}
-
-// One thread a row: its numbers out of the parts' sums.
-template <DType T, bool REF>
-__global__ void __launch_bounds__(64) row_finish_kernel(RowArgs a, RowCoef *coef, int S, int per) {
-    const long i = (long)blockIdx.x * 64 + threadIdx.x;
-    if (i >= a.N) return;
-    RowStats r = {};
-    if (row_counts(a, i)) r = join_parts<REF>(a, i, S, per, Chunk<T>::N);
-    float logp, entropy;
-    double terms[4];
-    const RowCoef c = row_numbers(a, i, r, logp, entropy, terms);
-    if (a.logp != nullptr) a.logp[i] = logp;
-    if (a.entropy != nullptr) a.entropy[i] = entropy;
-    if (!a.policy) return;
-    coef[i] = c;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a.row_terms[i * 4 + k] = terms[k];
-}
-
 // The gradient of one chunk, without the token's own term.
 template <DType T, bool REF>
-__device__ __forceinline__ void grad_chunk(const RowCoef &r, const uint4 &zc, const uint4 &qc, float kz, float kq, float *g) {
+__device__ __forceinline__ void grad_chunk(const RowCoef &r, const uint4 &zc, const uint4 &qc, float *g) {
     constexpr int N = Chunk<T>::N;
     float z[N], q[N];
     unpack_frag<T>(zc, z);
     if (REF) unpack_frag<T>(qc, q);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float x = (z[k] - r.M) * kz, e = __builtin_amdgcn_exp2f(x);
-        float in = r.A * x + r.B;
-        if (REF) in += r.C * (x - (q[k] - r.Mq) * kq);
+        const float x = r.z.of(z[k]), e = __builtin_amdgcn_exp2f(x);
+        float in = fmaf(r.A, x, r.B);
+        if (REF) in = fmaf(-r.C, r.q.of(q[k]), in);
         g[k] = mul0(e, in);
     }
 }
@@ -318,203 +383,318 @@ __device__ __forceinline__ void add_token(float *g, int k0, float v) {
     for (int k = 0; k < Chunk<T>::N; ++k) g[k] += k == k0 ? v : 0.f;
 }
 
-template <DType T, bool REF>
-__global__ void __launch_bounds__(kRowThreads) row_grad_kernel(RowArgs a, const RowCoef *coef, int S, int per) {
-    typedef typename St<T>::type E;
-    const long i = blockIdx.x / S;
-    const int p = (int)(blockIdx.x - i * S);
-    const E *z = (const E *)a.z + i * a.ldz;
-    const E *q = REF ? (const E *)a.q + i * a.ldq : nullptr;
-    E *dz = (E *)a.dz + i * a.lddz;
-    const int nch = (a.V + Chunk<T>::N - 1) / Chunk<T>::N;
-    const int c1 = min(nch, (p + 1) * per);
-    const RowCoef r = coef[i];
-    const int at = a.tok[i];
-    for (int c = p * per + threadIdx.x; c < c1; c += kRowThreads) {
-        float g[Chunk<T>::N];
-        if (r.dead != 0.f) {
-#pragma unroll
-            for (int k = 0; k < Chunk<T>::N; ++k) g[k] = 0.f;
-        } else {
-            const uint4 zc = Chunk<T>::load(z, c, a.V), qc = REF ? Chunk<T>::load(q, c, a.V) : zc;
-            grad_chunk<T, REF>(r, zc, qc, a.kz, a.kq, g);
-            if (c == at / Chunk<T>::N) add_token<T>(g, at % Chunk<T>::N, r.at);
-        }
-        Chunk<T>::store(dz, c, a.V, g);
-    }
-}
-
-// One workgroup a row, the row in registers: read once, its maximum, its sums, its numbers, its gradient
-// written.  Thread t holds chunks t, t + NT, ...; NT NC of them at most, and with BIG those past that are
-// read twice, once for the sums with running maxima and once (from the last-level cache) for the gradient.
-template <DType T, bool REF, int NT, int NC, bool BIG>
-__global__ void __launch_bounds__(NT) row_fused_kernel(RowArgs a) {
-    typedef typename St<T>::type E;
-    constexpr int N = Chunk<T>::N, NW = NT / 64;
-    __shared__ float redm[2][NW], reds[4][NW];
-    __shared__ RowCoef coef;
-    const long i = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int nfull = a.V / N, nch = (a.V + N - 1) / N;
-    E *dz = (E *)a.dz + i * a.lddz;
-    if (!row_counts(a, i)) {
-        if (a.dz != nullptr) {
-            const float zero[N] = {};
-            for (int c = tid; c < nch; c += NT) Chunk<T>::store(dz, c, a.V, zero);
-        }
-        if (tid == 0) {
-            if (a.logp != nullptr) a.logp[i] = 0.f;
-            if (a.entropy != nullptr) a.entropy[i] = 0.f;
-            if (a.policy)
-                for (int k = 0; k < 4; ++k) a.row_terms[i * 4 + k] = 0.0;
-        }
-        return;
-    }
-    const E *z = (const E *)a.z + i * a.ldz;
-    const E *q = REF ? (const E *)a.q + i * a.ldq : nullptr;
-    const float kz = a.kz, kq = a.kq;
-    const uint4 none = uint4{Chunk<T>::kNegInf, Chunk<T>::kNegInf, Chunk<T>::kNegInf, Chunk<T>::kNegInf};
-    uint4 zr[NC], qr[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {  // all loads in flight; past the row the last whole chunk again, replaced below
-        zr[c] = none;
-        if (REF) qr[c] = none;
-        if (c * NT < nfull) {
-            const size_t at = (size_t)min(tid + c * NT, nfull - 1) * N;
-            zr[c] = ld16(z + at);
-            if (REF) qr[c] = ld16(q + at);
-        }
-    }
-    const int at = a.tok[i];
-    const float za = St<T>::load(z, at);
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-        if (c * NT < nch && (c + 1) * NT > nfull) {  // where the row ends
-            const int cc = tid + c * NT;
-            if (cc >= nfull) {
-                zr[c] = none;
-                if (REF) qr[c] = none;
-                if (cc < nch) {
-                    zr[c] = Chunk<T>::load(z, cc, a.V);
-                    if (REF) qr[c] = Chunk<T>::load(q, cc, a.V);
-                }
-            }
-        }
-    RowStats r = {kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, za, 0.f};
-    if (BIG) {
-        constexpr int U = REF ? 2 : 4;
-        for (int c = NC * NT + tid; c < nch; c += NT * U) {
-            uint4 zc[U], qc[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int cc = c + u * NT < nch ? c + u * NT : c;
-                zc[u] = Chunk<T>::load(z, cc, a.V);
-                if (REF) qc[u] = Chunk<T>::load(q, cc, a.V);
-            }
-            float M = r.M, Mq = r.Mq;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                M = fmaxf(M, chunk_max<T>(zc[u]));
-                if (REF) Mq = fmaxf(Mq, chunk_max<T>(qc[u]));
-            }
-            rebase<REF>(r, M, Mq, kz, kq);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (c + u * NT < nch) add_chunk<T, REF>(r, zc[u], REF ? qc[u] : zc[u], kz, kq);
-        }
-    }
-    float M = r.M, Mq = r.Mq;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-        if (c * NT < nch) {
-            M = fmaxf(M, chunk_max<T>(zr[c]));
-            if (REF) Mq = fmaxf(Mq, chunk_max<T>(qr[c]));
-        }
-    M = wave_max(M);
-    if (REF) Mq = wave_max(Mq);
-    if (NW > 1) {
-        if (lane == 0) {
-            redm[0][w] = M;
-            if (REF) redm[1][w] = Mq;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < NW; ++k) {
-            M = fmaxf(M, redm[0][k]);
-            if (REF) Mq = fmaxf(Mq, redm[1][k]);
-        }
-    }
-    if (BIG) {
-        rebase<REF>(r, M, Mq, kz, kq);
-    } else {
-        r.M = M;
-        r.Mq = Mq;
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-        if (c * NT < nch) add_chunk<T, REF>(r, zr[c], REF ? qr[c] : zr[c], kz, kq);
+template <bool REF>
+__device__ __forceinline__ void sum_lanes(RowStats &r) {
     r.s = wave_sum(r.s);
     r.t = wave_sum(r.t);
     if (REF) {
         r.k = wave_sum(r.k);
         r.sq = wave_sum(r.sq);
     }
+}
+
+// The workgroup's threads' sums as one, in a fixed order, in every lane of wave 0 (other waves: anything).
+// A row whose largest probability is close to 1 has its logarithm in what the other tokens add, which a sum
+// that holds the largest itself would round away: where the whole is below 1.5 times that (so that one thread alone
+// has the maximum, once), that thread's chunks are read again and added without it; s is then the sum of the
+// others, and top 1.  Thread t's chunks are first + t, first + t + NT, ... below last.
+template <DType T, bool REF, int NT>
+__device__ __forceinline__ RowStats join_threads(RowStats r, const RowArgs &a, const Row<T> &row, int first, int last) {
+    constexpr int NW = NT / 64, N = Chunk<T>::N;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const float M = wave_max(r.M), Mq = REF ? wave_max(r.Mq) : kLowest;
+    const bool mine = r.M == M;
+    rebase<REF>(r, M, Mq, a.kz, a.kq);
+    float other = wave_sum(mine ? 0.f : r.s), who = wave_max(mine ? (float)threadIdx.x : -1.f);
+    sum_lanes<REF>(r);
     if (NW > 1) {
+        __shared__ RowStats waves[NW];
+        __shared__ float others[NW], whos[NW];
         if (lane == 0) {
-            reds[0][w] = r.s;
-            reds[1][w] = r.t;
-            if (REF) {
-                reds[2][w] = r.k;
-                reds[3][w] = r.sq;
-            }
+            waves[w] = r;
+            others[w] = other;
+            whos[w] = who;
         }
         __syncthreads();
+        if (w != 0) return r;
+        const int l = lane & (NW - 1);
+        const bool in = lane < NW;
+        const float za = r.za;
+        r = waves[l];
+        r.za = za;
+        const float Mw = wave_max(r.M), Mqw = REF ? wave_max(r.Mq) : kLowest;
+        const bool has = r.M == Mw;
+        rebase<REF>(r, Mw, Mqw, a.kz, a.kq);
+        other = wave_sum(in ? (has ? others[l] : r.s) : 0.f);
+        who = wave_max(in && has ? whos[l] : -1.f);
+        if (!in) r.s = r.t = r.k = r.sq = 0.f;
+        sum_lanes<REF>(r);
     }
-    if (w == 0) {
-        if (NW > 1) {
-            r.s = wave_sum(lane < NW ? reds[0][lane & (NW - 1)] : 0.f);
-            r.t = wave_sum(lane < NW ? reds[1][lane & (NW - 1)] : 0.f);
-            if (REF) {
-                r.k = wave_sum(lane < NW ? reds[2][lane & (NW - 1)] : 0.f);
-                r.sq = wave_sum(lane < NW ? reds[3][lane & (NW - 1)] : 0.f);
+    const Scale sz = scale_of(r.M, a.kz);
+    if (r.s < 1.5f * __builtin_amdgcn_exp2f(sz.of(r.M)) && r.s > 0.f) {
+        float own = 0.f;
+        for (int c = first + (int)who + lane * NT; c < last; c += 64 * NT) {
+            float v[N];
+            unpack_frag<T>(row.any(row.z, c), v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) own += v[k] == r.M ? 0.f : __builtin_amdgcn_exp2f(sz.of(v[k]));
+        }
+        r.s = other + wave_sum(own);
+        r.top = 1.f;
+    }
+    return r;
+}
+
+// Wave 0 of a row's workgroup: its numbers out of its sums, and the outputs that are one a row.
+__device__ __forceinline__ RowCoef finish_row(const RowArgs &a, long i, const RowIn &in, const RowStats &r, bool out) {
+    float logp, entropy;
+    double terms[4];
+    const RowCoef c = row_numbers(a, in, r, logp, entropy, terms);
+    if (out && threadIdx.x == 0) {
+        if (a.logp != nullptr) a.logp[i] = logp;
+        if (a.entropy != nullptr) a.entropy[i] = entropy;
+        if (a.policy)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a.row_terms[i * 4 + k] = terms[k];
+    }
+    return c;
+}
+__device__ __forceinline__ void mask_row(const RowArgs &a, long i) {
+    if (threadIdx.x != 0) return;
+    if (a.logp != nullptr) a.logp[i] = 0.f;
+    if (a.entropy != nullptr) a.entropy[i] = 0.f;
+    if (a.policy)
+        for (int k = 0; k < 4; ++k) a.row_terms[i * 4 + k] = 0.0;
+}
+
+// The gradient of chunk c of a row.
+template <DType T, bool REF>
+__device__ __forceinline__ uint4 grad_of(const RowCoef &r, int c, int at, const uint4 &zc, const uint4 &qc) {
+    constexpr int N = Chunk<T>::N;
+    if (r.dead != 0.f) return uint4{0u, 0u, 0u, 0u};
+    float g[N];
+    if (REF && r.C != 0.f)
+        grad_chunk<T, REF>(r, zc, qc, g);
+    else
+        grad_chunk<T, false>(r, zc, zc, g);
+    if (c == at / N) add_token<T>(g, at % N, r.at);
+    return pack_frag_cvt<T>(g);
+}
+
+// One workgroup a row, read once: thread t holds chunks t, t + NT, ... from the first look to the gradient,
+// NC of them in registers and the next SL in LDS.  With BIG there are more, which are read twice: for the
+// sums, and (from the last-level cache) for the gradient.  The sums run with each thread's own maximum, as
+// the loads arrive.  NC = 0: no gradient is wanted, and nothing is held.
+template <DType T, bool REF, int NT, int NC, int SL, bool BIG>
+__global__ void __launch_bounds__(NT) row_kernel(RowArgs a) {
+    typedef typename St<T>::type E;
+    constexpr int N = Chunk<T>::N, R = NC > 0 ? NC : 1, P = REF ? 2 : 1;
+    __shared__ RowCoef coef;
+    extern __shared__ uint4 kept[];  // [SL][P][NT]
+    const long i = blockIdx.x;
+    const int tid = threadIdx.x;
+    const RowIn in = row_in(a, i);
+    const Row<T> row(a, i, in.tok, REF);
+    const int nfull = row.nfull, nch = row.nch;
+    if (!in.counts) {
+        if (NC > 0)
+            for (int c = tid; c < nch; c += NT) row.store(c, uint4{0u, 0u, 0u, 0u});
+        mask_row(a, i);
+        return;
+    }
+    const uint4 none = uint4{Chunk<T>::kNegInf, Chunk<T>::kNegInf, Chunk<T>::kNegInf, Chunk<T>::kNegInf};
+    uint4 zr[R], qr[R];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {  // all loads in flight; past the whole chunks the last one again
+        zr[c] = none;
+        if (REF) qr[c] = none;
+        if (c * NT < nfull) {
+            const int cc = min(tid + c * NT, nfull - 1);
+            zr[c] = row.template load<true>(row.z, cc);
+            if (REF) qr[c] = row.template load<true>(row.q, cc);
+        }
+    }
+    RowStats r = {kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, St<T>::load(row.z, row.at), 0.f};
+    if (NC > 0 && T == DType::BF16 && row.lead && tid == 0) {
+        row.first(zr[0]);
+        if (REF) row.first(qr[0]);
+    }
+    if (BIG) {
+        constexpr int U = REF ? 2 : 4;
+        static_assert(SL % U == 0, "a round of loads is kept whole or not at all");
+        // chunks c, c + NT, ...: U of them, kept from the given slot on (or not: -1), read once or twice
+        auto round = [&](int c, int slot, auto once) __attribute__((always_inline)) {
+            constexpr bool ONCE = decltype(once)::value;
+            uint4 zc[U], qc[U];
+            bool used[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                used[u] = c + u * NT < nfull;
+                const int cc = min(c + u * NT, nfull - 1);
+                zc[u] = row.template load<ONCE>(row.z, cc);
+                if (REF) qc[u] = row.template load<ONCE>(row.q, cc);
             }
-        }
-        float logp, entropy;
-        double terms[4];
-        const RowCoef c = row_numbers(a, i, r, logp, entropy, terms);
-        if (lane == 0) {
-            coef = c;
-            if (a.logp != nullptr) a.logp[i] = logp;
-            if (a.entropy != nullptr) a.entropy[i] = entropy;
-            if (a.policy)
+            if (NC == 0 && T == DType::BF16 && row.lead && c == 0) {
+                row.first(zc[0]);
+                if (REF) row.first(qc[0]);
+            }
+            if (slot >= 0) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) a.row_terms[i * 4 + k] = terms[k];
+                for (int u = 0; u < U; ++u) {
+                    kept[((slot + u) * P) * NT + tid] = zc[u];
+                    if (REF) kept[((slot + u) * P + 1) * NT + tid] = qc[u];
+                }
+            }
+            add_chunks<T, REF, U>(r, zc, REF ? qc : zc, used, a.kz, a.kq);
+        };
+        int c = NC * NT + tid;
+#pragma unroll 1
+        for (int slot = 0; slot < SL && c < nfull; slot += U, c += NT * U) round(c, slot, std::true_type{});
+#pragma unroll 1
+        for (; c < nfull; c += NT * U) round(c, -1, std::integral_constant<bool, NC == 0>{});
+    }
+    // one chunk at a time with a reference (two hold more registers: 32000 entries in bf16 95 -> 105 us), else two
+    constexpr int G = REF ? 1 : 2;
+    static_assert(NC % G == 0, "whole groups");
+#pragma unroll
+    for (int c = 0; c < NC; c += G)
+        if (c * NT < nfull) {
+            bool used[G];
+#pragma unroll
+            for (int u = 0; u < G; ++u) used[u] = tid + (c + u) * NT < nfull;
+            // the second of a group may lie wholly past the row and hold -inf, which adds nothing
+            add_chunks<T, REF, G>(r, zr + c, REF ? qr + c : zr + c, used, a.kz, a.kq);
+        }
+    const bool ends = nfull < nch && tid == nfull % NT;  // the row's last elements are this thread's
+    if (ends) {
+        const uint4 zt = Chunk<T>::tail(row.z, row.V), qt = REF ? Chunk<T>::tail(row.q, row.V) : none;
+        const bool used = true;
+        add_chunks<T, REF, 1>(r, &zt, &qt, &used, a.kz, a.kq);
+    }
+    r = join_threads<T, REF, NT>(r, a, row, 0, nch);
+    if (tid < 64) {
+        const RowCoef c = finish_row(a, i, in, r, true);
+        if (tid == 0) coef = c;
+    }
+    if (NC == 0) return;
+    __syncthreads();
+    const RowCoef rc = uniform(coef);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        const int cc = tid + c * NT;
+        if (cc < nfull) {
+            const uint4 g = grad_of<T, REF>(rc, cc, row.at, zr[c], REF ? qr[c] : zr[c]);
+            if (c == 0)
+                row.store(cc, g);
+            else
+                st16_once((uint8_t *)row.dz + (uint32_t)cc * 16u, g);
         }
     }
-    if (a.dz == nullptr) return;
-    __syncthreads();
-    const RowCoef rc = coef;
-    const bool dead = rc.dead != 0.f, kl = REF && rc.C != 0.f;
-    auto put = [&](int c, const uint4 &zc, const uint4 &qc) {  // chunk c of the row
-        float g[N];
-        if (dead) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) g[k] = 0.f;
-        } else {
-            if (kl)
-                grad_chunk<T, REF>(rc, zc, qc, kz, kq, g);
-            else
-                grad_chunk<T, false>(rc, zc, zc, kz, kq, g);
-            if (c == at / N) add_token<T>(g, at % N, rc.at);
+    if (BIG) {
+        int c = NC * NT + tid;
+        for (int slot = 0; slot < SL && c < nfull; ++slot, c += NT)
+            st16_once((uint8_t *)row.dz + (uint32_t)c * 16u,
+                      grad_of<T, REF>(rc, c, row.at, kept[slot * P * NT + tid], kept[(slot * P + P - 1) * NT + tid]));
+        for (; c < nfull; c += NT) {
+            const uint4 zc = row.template load<false>(row.z, c), qc = REF ? row.template load<false>(row.q, c) : zc;
+            st16_once((uint8_t *)row.dz + (uint32_t)c * 16u, grad_of<T, REF>(rc, c, row.at, zc, qc));
         }
-        Chunk<T>::store(dz, c, a.V, g);
-    };
+    }
+    if (ends) {
+        const uint4 zt = Chunk<T>::tail(row.z, row.V), qt = REF ? Chunk<T>::tail(row.q, row.V) : none;
+        Chunk<T>::store_tail(row.dz, row.V, grad_of<T, REF>(rc, nfull, row.at, zt, qt));
+    }
+}
+
+// Few rows: each split over S workgroups (S <= 64), two launches.  The first leaves the sums of every part, the
+// second joins a row's parts in each of its workgroups (wave 0, a lane a part) and writes their gradients.
+// The first's loads stay in the caches for the second.
+constexpr int kPartThreads = 256;
+
+template <DType T, bool REF>
+__global__ void __launch_bounds__(kPartThreads) row_part_kernel(RowArgs a, int S, int per) {
+    typedef typename St<T>::type E;
+    constexpr int N = Chunk<T>::N, NT = kPartThreads, U = 2;
+    const long i = blockIdx.x / S;
+    const int p = (int)(blockIdx.x - i * S), tid = threadIdx.x;
+    const RowIn in = row_in(a, i);
+    if (!in.counts) return;
+    const Row<T> row(a, i, in.tok, REF);
+    const int first = p * per, last = min(row.nch, first + per), whole = min(row.nfull, last);
+    const int own = row.at / N;
+    RowStats r = {kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, own >= first && own < last ? St<T>::load(row.z, row.at) : 0.f, 0.f};
+    for (int c = first + tid; c < whole; c += NT * U) {
+        uint4 zc[U], qc[U];
+        bool used[U];
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-        if (tid + c * NT < nch) put(tid + c * NT, zr[c], REF ? qr[c] : zr[c]);
-    if (BIG)
-        for (int c = NC * NT + tid; c < nch; c += NT)
-            put(c, Chunk<T>::load(z, c, a.V), REF ? Chunk<T>::load(q, c, a.V) : none);
+        for (int u = 0; u < U; ++u) {
+            used[u] = c + u * NT < whole;
+            const int cc = min(c + u * NT, whole - 1);
+            zc[u] = row.template load<false>(row.z, cc);
+            if (REF) qc[u] = row.template load<false>(row.q, cc);
+        }
+        if (T == DType::BF16 && row.lead && c == 0) {
+            row.first(zc[0]);
+            if (REF) row.first(qc[0]);
+        }
+        add_chunks<T, REF, U>(r, zc, REF ? qc : zc, used, a.kz, a.kq);
+    }
+    if (last > row.nfull && first <= row.nfull && tid == (row.nfull - first) % NT) {  // the row's end is in this part
+        const uint4 zt = Chunk<T>::tail(row.z, row.V), qt = REF ? Chunk<T>::tail(row.q, row.V) : zt;
+        const bool used = true;
+        add_chunks<T, REF, 1>(r, &zt, &qt, &used, a.kz, a.kq);
+    }
+    r = join_threads<T, REF, NT>(r, a, row, first, last);
+    if (tid == 0) a.part[i * S + p] = r;
+}
+
+// The parts of row i as one, a lane of the wave a part.  What is left out of a part's s (its top) stays out
+// only where it is the row's maximum.
+template <bool REF>
+__device__ __forceinline__ RowStats join_parts(const RowArgs &a, long i, int S, int own) {
+    const int lane = threadIdx.x & 63;
+    const bool in = lane < S;
+    RowStats r = a.part[i * S + min(lane, S - 1)];
+    const float M = wave_max(r.M), Mq = REF ? wave_max(r.Mq) : kLowest;
+    if (r.M != M) {
+        r.s += r.top * __builtin_amdgcn_exp2f(scale_of(r.M, a.kz).of(r.M));
+        r.top = 0.f;
+    }
+    rebase<REF>(r, M, Mq, a.kz, a.kq);
+    if (!in) r.s = r.t = r.k = r.sq = r.top = 0.f;
+    sum_lanes<REF>(r);
+    r.top = wave_sum(r.top);
+    r.za = lane_f32(r.za, __builtin_amdgcn_readfirstlane(own));
+    return r;
+}
+
+template <DType T, bool REF, bool GRAD>
+__global__ void __launch_bounds__(kPartThreads) row_rest_kernel(RowArgs a, int S, int per) {
+    typedef typename St<T>::type E;
+    constexpr int N = Chunk<T>::N, NT = kPartThreads;
+    __shared__ RowCoef coef;
+    const long i = GRAD ? blockIdx.x / S : blockIdx.x;
+    const int p = (int)(blockIdx.x - i * S), tid = threadIdx.x;
+    const RowIn in = row_in(a, i);
+    const Row<T> row(a, i, in.tok, REF);
+    const int first = p * per, last = min(row.nch, first + per);
+    if (!in.counts) {
+        if (GRAD)
+            for (int c = first + tid; c < last; c += NT) row.store(c, uint4{0u, 0u, 0u, 0u});
+        if (!GRAD || p == 0) mask_row(a, i);
+        return;
+    }
+    if (tid < 64) {
+        const RowCoef c = finish_row(a, i, in, join_parts<REF>(a, i, S, row.at / N / per), !GRAD || p == 0);
+        if (tid == 0) coef = c;
+    }
+    if (!GRAD) return;
+    __syncthreads();
+    const RowCoef rc = uniform(coef);
+    for (int c = first + tid; c < last; c += NT) {
+        const uint4 zc = row.any(row.z, c), qc = REF ? row.any(row.q, c) : zc;
+        row.store(c, grad_of<T, REF>(rc, c, row.at, zc, qc));
+    }
 }
 
 // The loss and its terms, the rows in a fixed order.
@@ -542,74 +722,87 @@ __global__ void __launch_bounds__(1024) row_terms_kernel(RowArgs a) {
     a.terms[0] = (float)(s[0] + (a.c_kl != 0.0 ? a.c_kl * s[1] : 0.0) - a.c_ent * s[2]);
 }
 
-// Parts of a row: enough workgroups for the chip where there are few rows, but at least one round of
-// loads (kRowThreads * kRowUnroll chunks) each.
-static int row_parts(long N, int nch, int &per) {
-    const int most = (nch + kRowThreads * kRowUnroll - 1) / (kRowThreads * kRowUnroll);
-    const long want = (4L * compute_units() + N - 1) / N;
-    int S = (int)(want < most ? want : most);
-    per = (nch + S - 1) / S;
+static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Parts of a row of nch chunks: 1 where its workgroup does the whole row.  (SPLITTING RULE)
+static int row_parts(long N, int nch, bool grad, int &per) {
+    const int cu = compute_units();
+    per = nch;
+    if (N <= 0 || 4 * N > cu || nch < (grad ? 4096 : 16384)) return 1;
+    const long want = std::min<long>(64, std::min<long>(2L * cu / N, (nch + kPartThreads - 1) / kPartThreads));
+    if (want < 2) return 1;
+    per = (int)((nch + want - 1) / want);
+    per = (per + kPartThreads - 1) / kPartThreads * kPartThreads;
     return (nch + per - 1) / per;
 }
 
-static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 size_t rows_workspace(long N, int V, bool policy) {
     int per;
-    const int S = row_parts(N > 0 ? N : 1, (V + 3) / 4, per);
-    return up256((size_t)N * S * sizeof(RowStats)) + (policy ? up256((size_t)N * 32) + up256((size_t)N * sizeof(RowCoef)) : 0);
+    const int S = row_parts(N, (V + 3) / 4, policy, per);  // as many chunks as any type has
+    return (S > 1 ? up256((size_t)N * 64 * sizeof(RowStats)) : 0) + (policy ? up256((size_t)N * 32) : 0);
 }
 
-// Whether a row is one workgroup's (row_fused_kernel) or is split over several.
-static bool row_whole(long N, int V) { return true; }
+template <DType T, bool REF, int NT, int NC, int SL = 0, bool BIG = false>
+static void launch_row_shape(const RowArgs &a, hipStream_t s) {
+    constexpr int lds = SL * (REF ? 2 : 1) * NT * 16;
+    if (lds > 0) {
+        static const hipError_t set = hipFuncSetAttribute((const void *)row_kernel<T, REF, NT, NC, SL, BIG>,
+                                                          hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        (void)set;
+    }
+    row_kernel<T, REF, NT, NC, SL, BIG><<<(unsigned)a.N, NT, lds, s>>>(a);
+}
 
+// The workgroup that holds a row of nch chunks.  (SHAPES)
 template <DType T, bool REF>
-static void launch_fused(const RowArgs &a, int nch, hipStream_t s) {
-    const unsigned n = (unsigned)a.N;
-    if (nch <= 64 * 4)
-        row_fused_kernel<T, REF, 64, 4, false><<<n, 64, 0, s>>>(a);
-    else if (nch <= 256 * 4)
-        row_fused_kernel<T, REF, 256, 4, false><<<n, 256, 0, s>>>(a);
-    else if (nch <= 256 * 8)
-        row_fused_kernel<T, REF, 256, 8, false><<<n, 256, 0, s>>>(a);
-    else if (nch <= 512 * 8)
-        row_fused_kernel<T, REF, 512, 8, false><<<n, 512, 0, s>>>(a);
-    else if (nch <= 1024 * 8)
-        row_fused_kernel<T, REF, 1024, 8, false><<<n, 1024, 0, s>>>(a);
-    else
-        row_fused_kernel<T, REF, 1024, 8, true><<<n, 1024, 0, s>>>(a);
+static void launch_row(const RowArgs &a, int nch, hipStream_t s) {
+    if (a.dz == nullptr) {
+        if (nch <= 64 * 8)
+            launch_row_shape<T, REF, 64, 0, 0, true>(a, s);
+        else if (a.N >= 512)
+            launch_row_shape<T, REF, 256, 0, 0, true>(a, s);
+        else
+            launch_row_shape<T, REF, 1024, 0, 0, true>(a, s);
+    } else if (nch <= 64 * 4) {
+        launch_row_shape<T, REF, 64, 4>(a, s);
+    } else if (nch <= 256 * 4) {
+        launch_row_shape<T, REF, 256, 4>(a, s);
+    } else if (nch <= 256 * 8) {
+        launch_row_shape<T, REF, 256, 8>(a, s);
+    } else if (nch <= 512 * 8) {
+        launch_row_shape<T, REF, 512, 8>(a, s);
+    } else if constexpr (REF) {
+        if (nch <= 1024 * 8)
+            launch_row_shape<T, REF, 1024, 8>(a, s);
+        else
+            launch_row_shape<T, REF, 1024, 8, 4, true>(a, s);
+    } else {
+        if (nch <= 512 * 16)
+            launch_row_shape<T, REF, 512, 16>(a, s);
+        else if (nch <= 1024 * 16)
+            launch_row_shape<T, REF, 1024, 16>(a, s);
+        else
+            launch_row_shape<T, REF, 1024, 16, 8, true>(a, s);
+    }
 }
 
 template <DType T, bool REF>
 static void launch_rows_t(RowArgs a, void *workspace, hipStream_t s) {
-    const int nch = (a.V + Chunk<T>::N - 1) / Chunk<T>::N;
-    if (a.N > 0 && row_whole(a.N, a.V)) {
-        a.row_terms = (double *)workspace;
-        launch_fused<T, REF>(a, nch, s);
-        if (a.policy) row_terms_kernel<<<1, 1024, 0, s>>>(a);
-        return;
-    }
+    const int nch = (a.V + (T == DType::BF16 ? 1 : 0) + Chunk<T>::N - 1) / Chunk<T>::N;  // with a lead
     int per;
-    const int S = row_parts(a.N > 0 ? a.N : 1, nch, per);
-    uint8_t *w = (uint8_t *)workspace;
-    a.part = (RowStats *)w;
-    w += up256((size_t)a.N * S * sizeof(RowStats));
-    a.row_terms = (double *)w;
-    RowCoef *coef = (RowCoef *)(w + up256((size_t)a.N * 32));
-    if (a.N == 0) {  // no rows: the terms are 0
-        row_terms_kernel<<<1, 1024, 0, s>>>(a);
-        return;
-    }
-    row_stats_kernel<T, REF><<<(unsigned)(a.N * S), kRowThreads, 0, s>>>(a, S, per);
-    row_finish_kernel<T, REF><<<(unsigned)((a.N + 63) / 64), 64, 0, s>>>(a, coef, S, per);
-    if (!a.policy) return;
-    if (a.dz != nullptr) {
-        if (REF && a.c_kl != 0.0)
-            row_grad_kernel<T, REF><<<(unsigned)(a.N * S), kRowThreads, 0, s>>>(a, coef, S, per);
+    const int S = row_parts(a.N, nch, a.dz != nullptr, per);
+    a.row_terms = (double *)workspace;
+    a.part = (RowStats *)((uint8_t *)workspace + (a.policy ? up256((size_t)a.N * 32) : 0));
+    if (a.N > 0 && S == 1) {
+        launch_row<T, REF>(a, nch, s);
+    } else if (a.N > 0) {
+        row_part_kernel<T, REF><<<(unsigned)(a.N * S), kPartThreads, 0, s>>>(a, S, per);
+        if (a.dz != nullptr)
+            row_rest_kernel<T, REF, true><<<(unsigned)(a.N * S), kPartThreads, 0, s>>>(a, S, per);
         else
-            row_grad_kernel<T, false><<<(unsigned)(a.N * S), kRowThreads, 0, s>>>(a, coef, S, per);
+            row_rest_kernel<T, REF, false><<<(unsigned)a.N, 64, 0, s>>>(a, S, per);
     }
-    row_terms_kernel<<<1, 1024, 0, s>>>(a);
+    if (a.policy) row_terms_kernel<<<1, 1024, 0, s>>>(a);
 }
 
 void launch_rows(DType t, RowArgs a, void *workspace, hipStream_t s) {

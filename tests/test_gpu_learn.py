@@ -270,6 +270,63 @@ def test_rows_that_are_masked(V, ref, dtype):
     assert (none.grad == 0).all() and (none.terms == 0).all()
 
 
+@pytest.mark.parametrize("ref", ["none", "logits"])
+@pytest.mark.parametrize("offset", [-1e4, 1e5, -1e6, 3e7])
+@pytest.mark.parametrize("V", [50, 3000, 33000])
+def test_logits_far_from_zero(V, offset, ref):
+    """All of a row's logits moved by one number, by which fp32 leaves them whole steps of 2^-10 to 2: nothing
+    is lost that is still there."""
+    z, tok, d = make_policy(6, V, F32, ref, seed=11)
+    z += offset
+    d["old_logp"] = oracle(z, tok, d["advantages"])["logp"].float().cuda() + 0.01
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.0 if ref == "none" else 0.3, c_ent=0.02)
+    if ref == "logits":
+        d["ref_logits"] += -2 * offset
+    check_policy(learn().policy_loss(z, tok, **d, **kw), oracle(z, tok, **d, **kw), F32, V)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("mask", [-1e9, -1e10, -1e20, -1e30, -3e38])
+@pytest.mark.parametrize("V", [50, 9000, 70001])
+def test_masks_of_large_negative_numbers(V, mask, dtype):
+    """Half of every row at the mask, and one row wholly there, which is uniform."""
+    z, tok, d = make_policy(5, V, dtype, "logits", seed=13)
+    out = torch.rand(V, generator=torch.Generator().manual_seed(V)) < 0.5
+    out[tok.cpu().long()] = False
+    for t in (z, d["ref_logits"]):
+        t[:, out.cuda()] = mask
+        t[3] = mask
+    d["old_logp"] = (oracle(z, tok, d["advantages"])["logp"] + 0.05).float().cuda()
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.3, c_ent=0.02)
+    check_policy(learn().policy_loss(z, tok, **d, **kw), oracle(z, tok, **d, **kw), dtype, V)
+    lp, ent = learn().token_logprobs(z, tok, entropy=True)
+    assert abs(lp[3].item() + math.log(V)) <= tol(0, V) + U * math.log(V)
+    assert abs(ent[3].item() - math.log(V)) <= tol(0, V) * (1 + math.log(V))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(4, 63), (3, 5001), (700, 3001), (3, 131075), (80, 33333)])
+def test_likely_tokens_keep_their_digits(n, V, dtype):
+    """Rows whose largest logit leads by up to 30: the log-probability of its token is -log1p(rest), rest the
+    sum of the others' exponentials, and held relative to itself (with one rounding of the result to fp32).
+    The kernel adds rest to the largest in 64 bits and takes the logarithm: two roundings of 2^-53 there.  The
+    entropy's sum holds the largest logit's own x, which is the rounding of a product of up to 93 (half a
+    step of 2^-17), and rounds it twice by u of itself: 2 u 2^-18 = 2^-41."""
+    z, tok, g = make_rows(n, V, dtype, seed=17)
+    top = z.float().amax(-1, keepdim=True)
+    lead = torch.linspace(2.0, 30.0, n).cuda()[:, None]
+    tok = torch.randint(0, V, (n,), generator=g).to(torch.int32).cuda()
+    z.scatter_(1, tok.long()[:, None], (top + math.log(V) + lead).to(dtype))
+    lp, ent = learn().token_logprobs(z, tok, entropy=True)
+    away = z.double().gather(1, tok.long()[:, None]) - z.double()
+    e = torch.exp(-away).scatter_(1, tok.long()[:, None], 0.0)
+    rest = e.sum(-1)
+    want, H = -torch.log1p(rest), torch.log1p(rest) + (e * away).sum(-1) / (1 + rest)
+    t = tol(away.max().item(), V)
+    assert ((lp.double() - want).abs() <= (t + U) * want.abs() + 2.0 ** -52).all()
+    assert ((ent.double() - H).abs() <= 2 * (t + U) * H + 2.0 ** -41 + 2.0 ** -52).all()
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("V", [100, 40000])
 def test_numbers_that_are_not_finite_show(bad, V):

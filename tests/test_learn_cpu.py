@@ -103,6 +103,7 @@ def test_capacity_and_workspaces():
         assert getattr(lib, name + "_workspace_bytes")(-1, 100) == 0
     assert lib.dvi_token_logprobs(_logprob(rows=1 << 40), A, 1 << 20, None) == _abi.ERR_CAPACITY
     assert lib.dvi_policy_loss(_policy(rows=1 << 40), A, 1 << 20, None) == _abi.ERR_CAPACITY
+    assert lib.dvi_policy_loss(_policy(vocab=(1 << 28) + 1, ld=1 << 29, grad_ld=1 << 29), A, 1 << 20, None) == _abi.ERR_CAPACITY
     t, args = _adamw(max_norm=1.0)
     assert lib.dvi_adamw(t, 2, args, A, lib.dvi_adamw_workspace_bytes(2) - 1, None) == _abi.ERR_CAPACITY
     t, args = _adamw(tensor=dict(n=1 << 50))
