@@ -333,7 +333,7 @@ dvi_status dvi_policy_loss(const dvi_policy_args *args, void *workspace, size_t 
 
 /*
  * One AdamW step over n_tensors parameter tensors (HOST array of descriptors of contiguous DEVICE arrays
- * of n elements each; n may be 0, and all together at most 2^35), decoupled weight decay, step number step >= 1:
+ * of n elements each; n may be 0, and all together at most 2^33), decoupled weight decay, step number step >= 1:
  *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2
  *   p <- p - lr weight_decay p - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
  * max_norm > 0: the norm of all gradients together goes to grad_norm (NULL or DEVICE fp32 [1]); a norm

@@ -1578,7 +1578,7 @@ extern "C" dvi_status dvi_adamw(const dvi_adamw_tensor *tensors, int32_t n_tenso
         masters += d.master != nullptr;
         ++used;
         chunks += d.n > kMaxAdamElements ? kMaxAdamChunks + 1 : (d.n + kAdamChunk - 1) / kAdamChunk;
-        if (chunks > kMaxAdamChunks) return op_fail(DVI_ERR_CAPACITY, "more than 2^35 elements");
+        if (chunks > kMaxAdamChunks) return op_fail(DVI_ERR_CAPACITY, "more than 2^33 elements");
     }
     if (masters && masters != used) return op_fail(DVI_ERR_ARG, "some tensors have a master and some do not");
     if (used == 0 && g->max_norm == 0.0) return DVI_OK;

@@ -49,8 +49,9 @@ void launch_rows(DType t, RowArgs a, void *workspace, hipStream_t s);
 // ---- AdamW ----
 constexpr int kStateBlock = 256;   // elements of a tensor that share the scales of 8-bit states
 constexpr int kAdamTensors = 48;   // tensors of one launch: their table is a kernel argument (4 KiB)
-constexpr int kAdamChunk = 4096;   // elements of a tensor that a workgroup takes at a time
-constexpr int kNormGrid = 1024;    // workgroups, and so partial sums, of a launch of the norm
+constexpr int kAdamChunk = 1024;   // elements of a tensor that a workgroup takes at least
+constexpr int kNormChunk = 8192;   // elements that a workgroup of the norm takes at a time
+constexpr int kNormGrid = 2048;    // workgroups, and so partial sums, of a launch of the norm
 
 struct AdamTensor {
     long n;

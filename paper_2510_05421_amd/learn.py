@@ -21,11 +21,6 @@ def _refuse(msg):
     raise _abi.DVIError(_abi.ERR_ARG, msg)
 
 
-def _check(st):
-    if st != _abi.OK:
-        raise _abi.DVIError(st, _abi.load().dvi_op_error().decode())
-
-
 def _logits(t, name):
     if t.dim() != 2 or t.dtype not in _DTYPES or not t.is_cuda:
         _refuse("%s must be a 2-d float32 or bfloat16 tensor on a GPU" % name)
@@ -47,13 +42,23 @@ def _vector(t, name, rows, dtype, device):
     return t.data_ptr()
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream   # the handle alone: a Stream object costs 2 us
+
+
 def _call(device, fn, *args):
     """fn(*args, stream) on the device's current stream, with the device current."""
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+    at = device.index
+    if torch.cuda.current_device() == at:
+        st = fn(*args, _raw_stream(at))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+            st = fn(*args, _raw_stream(at))
+    if st != _abi.OK:
+        raise _abi.DVIError(st, _abi.load().dvi_op_error().decode())
+
+
+def _workspace(nbytes, device):
+    return (torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes) if nbytes else (None, 0)
 
 
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: float = 1.0,
@@ -69,10 +74,10 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, temperature: floa
     tok = _vector(tokens, "tokens", rows, torch.int32, dev)
     logp = torch.empty(rows, dtype=torch.float32, device=dev)
     ent = torch.empty(rows, dtype=torch.float32, device=dev) if entropy else None
-    ws = torch.empty(lib.dvi_token_logprobs_workspace_bytes(rows, vocab), dtype=torch.uint8, device=dev)
+    ws, nbytes = _workspace(lib.dvi_token_logprobs_workspace_bytes(rows, vocab), dev)
     args = _abi.LogprobArgs(rows, vocab, _DTYPES[logits.dtype], ptr, _ld(logits), tok, temperature, logp.data_ptr(),
                             ent.data_ptr() if entropy else None)
-    _call(dev, lib.dvi_token_logprobs, args, ws.data_ptr(), ws.numel())
+    _call(dev, lib.dvi_token_logprobs, args, ws.data_ptr() if nbytes else None, nbytes)
     return logp, ent
 
 
@@ -105,9 +110,10 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, advantages: torch.Te
     dev = logits.device
     if advantages is None:
         _refuse("advantages must be given")
-    vec = [_vector(t, name, rows, torch.int32 if name == "tokens" else torch.float32, dev)
-           for t, name in ((tokens, "tokens"), (advantages, "advantages"), (old_logp, "old_logp"), (weights, "weights"),
-                           (ref_logp, "ref_logp"))]
+    f32 = torch.float32
+    tok, adv = _vector(tokens, "tokens", rows, torch.int32, dev), _vector(advantages, "advantages", rows, f32, dev)
+    old, wts = _vector(old_logp, "old_logp", rows, f32, dev), _vector(weights, "weights", rows, f32, dev)
+    rlp = _vector(ref_logp, "ref_logp", rows, f32, dev)
     ref = None
     if ref_logits is not None:
         ref = _logits(ref_logits, "ref_logits")
@@ -123,12 +129,12 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, advantages: torch.Te
         _refuse("out is given without grad")
     logp = torch.empty(rows, dtype=torch.float32, device=dev)
     terms = torch.empty(5, dtype=torch.float32, device=dev)
-    ws = torch.empty(lib.dvi_policy_loss_workspace_bytes(rows, vocab), dtype=torch.uint8, device=dev)
-    args = _abi.PolicyArgs(rows, vocab, _DTYPES[logits.dtype], ptr, _ld(logits), vec[0], vec[1], vec[2], vec[3], ref,
-                           _ld(ref_logits) if ref is not None else 0, vec[4], temperature, ref_temperature, clip_low,
+    ws, nbytes = _workspace(lib.dvi_policy_loss_workspace_bytes(rows, vocab), dev)
+    args = _abi.PolicyArgs(rows, vocab, _DTYPES[logits.dtype], ptr, _ld(logits), tok, adv, old, wts, ref,
+                           _ld(ref_logits) if ref is not None else 0, rlp, temperature, ref_temperature, clip_low,
                            clip_high, c_kl, c_ent, out.data_ptr() if grad else None, _ld(out) if grad else 0,
                            logp.data_ptr(), terms.data_ptr())
-    _call(dev, lib.dvi_policy_loss, args, ws.data_ptr(), ws.numel())
+    _call(dev, lib.dvi_policy_loss, args, ws.data_ptr() if nbytes else None, nbytes)
     return PolicyLoss(terms, logp, out if grad else None)
 
 
@@ -182,8 +188,7 @@ class AdamW:
             _refuse("parameters and states must not overlap")
         self.grad_norm = torch.zeros(1, dtype=torch.float32, device=self.device) if max_norm > 0 else None
         lib = _abi.load()
-        self._ws = torch.empty(lib.dvi_adamw_workspace_bytes(len(self.params)) if max_norm > 0 else 0, dtype=torch.uint8,
-                               device=self.device)
+        self._ws, self._ws_bytes = _workspace(lib.dvi_adamw_workspace_bytes(len(self.params)) if max_norm > 0 else 0, self.device)
         self._table = (_abi.AdamwTensor * len(self.params))()
         self._sizes = [p.numel() for p in self.params]
         for i, (e, p) in enumerate(zip(self._table, self.params)):
@@ -218,5 +223,6 @@ class AdamW:
                               self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps, self.weight_decay,
                               self.max_norm, self.seed & 0xFFFFFFFFFFFFFFFF,
                               None if self.grad_norm is None else self.grad_norm.data_ptr())
-        _call(dev, _abi.load().dvi_adamw, self._table, len(self._sizes), args, self._ws.data_ptr(), self._ws.numel())
+        _call(dev, _abi.load().dvi_adamw, self._table, len(self._sizes), args,
+              self._ws.data_ptr() if self._ws_bytes else None, self._ws_bytes)
         self.step_count += 1
