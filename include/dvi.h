@@ -249,6 +249,49 @@ typedef struct {
 
 dvi_status dvi_update_drafter(dvi_ctx *ctx, const dvi_update_args *args, dvi_update_stats *stats);
 
+/*
+ * Clipped policy update of the drafter: dvi_update_drafter with the loss of dvi_policy_loss (below) over
+ * all valid replay rows instead of the policy-gradient term over the fresh ones, so that every row of the
+ * ring trains, however often it has been used:
+ *   loss = 1/n sum_i [ -min(ratio_i A_i, clip(ratio_i, 1 - clip_low, 1 + clip_high) A_i)
+ *                      + c_kl KL(p_i || q_i) - c_ent H(p_i) ]
+ *   A_i = c_pg (r_i - baseline),  ratio_i = p_i(a_i) / p_i^old(a_i),  q_i = softmax(logits^phi_i / tau)
+ * p^old is the drafter that logged the row: a row is fresh at the first update after it was logged (by
+ * either call), when the drafter is still that one, so its ratio is 1 there and its log-probability is
+ * kept for the updates that follow.  (Rows put in by dvi_write_buffer count as logged then, whatever their
+ * fresh flag.)  Everything else is as in dvi_update_drafter.  Allowed in READY.
+ */
+typedef struct {
+    float c_pg, c_kl, c_ent;
+    float clip_low, clip_high;
+    float tau, baseline;
+    float lr, beta1, beta2, eps;
+    int32_t opt_step;
+    float *grad_A_out;
+    float *grad_B_out;
+} dvi_policy_update_args;
+
+typedef struct {
+    float loss, policy, kl, entropy, clipped;  /* means over the rows; clipped: the share of clipped rows */
+    int32_t rows, accepted, fresh, fresh_accepted;
+} dvi_policy_update_stats;
+
+dvi_status dvi_update_policy(dvi_ctx *ctx, const dvi_policy_update_args *args, dvi_policy_update_stats *stats);
+
+/*
+ * The optimizer of both updates: NULL for the Adam of dvi_update_drafter (the default), or the step of
+ * dvi_adamw (below) over the two factors with these settings and the update's lr, beta1, beta2, eps and
+ * opt_step.  max_norm 0: no clipping; state_bits 32 or 8.  grad_A_out and grad_B_out receive the gradients
+ * before clipping.  Setting either clears the moments.  DVI_ERR_STATE during a step.
+ */
+typedef struct {
+    int32_t state_bits;
+    double weight_decay, max_norm;
+    uint64_t seed;
+} dvi_optimizer;
+
+dvi_status dvi_set_optimizer(dvi_ctx *ctx, const dvi_optimizer *opt);
+
 /* ---- learning operators on the caller's tensors --------------------------------------------
  *
  * What a drafter's training (Section 3.4) does apart from the replay ring, for rows and parameters

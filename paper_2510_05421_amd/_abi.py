@@ -43,6 +43,21 @@ class UpdateStats(ctypes.Structure):
                 ("rows", c_i32), ("accepted", c_i32), ("fresh", c_i32), ("fresh_accepted", c_i32)]
 
 
+class PolicyUpdateArgs(ctypes.Structure):
+    _fields_ = [("c_pg", c_f32), ("c_kl", c_f32), ("c_ent", c_f32), ("clip_low", c_f32), ("clip_high", c_f32),
+                ("tau", c_f32), ("baseline", c_f32), ("lr", c_f32), ("beta1", c_f32), ("beta2", c_f32), ("eps", c_f32),
+                ("opt_step", c_i32), ("grad_A_out", c_vp), ("grad_B_out", c_vp)]
+
+
+class PolicyUpdateStats(ctypes.Structure):
+    _fields_ = [("loss", c_f32), ("policy", c_f32), ("kl", c_f32), ("entropy", c_f32), ("clipped", c_f32),
+                ("rows", c_i32), ("accepted", c_i32), ("fresh", c_i32), ("fresh_accepted", c_i32)]
+
+
+class Optimizer(ctypes.Structure):
+    _fields_ = [("state_bits", c_i32), ("weight_decay", c_f64), ("max_norm", c_f64), ("seed", ctypes.c_uint64)]
+
+
 class LogprobArgs(ctypes.Structure):
     _fields_ = [("rows", c_i64), ("vocab", c_i32), ("dtype", c_i32), ("logits", c_vp), ("ld", c_i64), ("tokens", c_vp),
                 ("temperature", c_f64), ("logp", c_vp), ("entropy", c_vp)]
@@ -81,6 +96,8 @@ SIGNATURES = {
     "dvi_decode_steps": (c_i32, [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp]),
     "dvi_abort_step": (c_i32, [c_vp]),
     "dvi_update_drafter": (c_i32, [c_vp, ctypes.POINTER(UpdateArgs), ctypes.POINTER(UpdateStats)]),
+    "dvi_update_policy": (c_i32, [c_vp, ctypes.POINTER(PolicyUpdateArgs), ctypes.POINTER(PolicyUpdateStats)]),
+    "dvi_set_optimizer": (c_i32, [c_vp, ctypes.POINTER(Optimizer)]),
     "dvi_op_error": (ctypes.c_char_p, []),
     "dvi_token_logprobs_workspace_bytes": (c_size, [c_i64, c_i32]),
     "dvi_token_logprobs": (c_i32, [ctypes.POINTER(LogprobArgs), c_vp, c_size, c_vp]),

@@ -100,6 +100,10 @@ struct dvi_ctx {
     // update
     float *upd_Z, *upd_stats, *upd_dA, *upd_du, *upd_dup, *upd_dB, *upd_loss, *upd_u;
     float *mA, *vA, *mB, *vB;
+    float *ring_old, *pol_logp, *pol_terms;  // log-probabilities when logged, and now; the policy loss's terms
+    void *op_ws;                             // workspace of the policy loss and of the gradients' norm
+    bool adamw = false;                      // dvi_set_optimizer
+    dvi_optimizer opt{};
     // host mirror
     int state = S_CREATED;
     int B = 0, k_spec = 0, ar_mode = 0;
@@ -300,6 +304,10 @@ static size_t layout(dvi_ctx *x, const dvi_config &c, void *base) {
     float *vA = b.take<float>(V * r * 4);
     float *mB = b.take<float>(r * d * 4);
     float *vB = b.take<float>(r * d * 4);
+    float *ring_old = b.take<float>(R * 4);
+    float *pol_logp = b.take<float>(R * 4);
+    float *pol_terms = b.take<float>(8 * 4);
+    void *op_ws = b.take<void>(std::max(rows_workspace((long)R, (int)V, true), (size_t)kNormGrid * sizeof(double)));
     if (x && base) {
         x->L = Ls;
         x->emb = emb; x->head = head; x->final_norm = final_norm; x->rope = rope;
@@ -322,6 +330,7 @@ static size_t layout(dvi_ctx *x, const dvi_config &c, void *base) {
         x->upd_Z = upd_Z; x->upd_stats = upd_stats; x->upd_dA = upd_dA; x->upd_du = upd_du; x->upd_dup = upd_dup; x->upd_dB = upd_dB;
         x->upd_loss = upd_loss; x->upd_u = lora_u;
         x->mA = mA; x->vA = vA; x->mB = mB; x->vB = vB;
+        x->ring_old = ring_old; x->pol_logp = pol_logp; x->pol_terms = pol_terms; x->op_ws = op_ws;
     }
     return align_up(b.off);
 }
@@ -1241,17 +1250,18 @@ static bool own_memory(const dvi_ctx *x, const void *p) {
     return at.type == hipMemoryTypeDevice && at.device == x->dev;
 }
 
-extern "C" dvi_status dvi_update_drafter(dvi_ctx *x, const dvi_update_args *ua, dvi_update_stats *stats) {
-    if (!x || !ua) return DVI_ERR_ARG;
-    if (x->device_error) return fail(x, DVI_ERR_DEVICE, "context has a sticky device error");
-    if (x->state != S_READY) return fail(x, DVI_ERR_STATE, "update needs state READY");
-    if (!(ua->tau > 0.f)) return fail(x, DVI_ERR_ARG, "tau must be > 0");
-    if (ua->lr != 0.f && ua->opt_step < 1) return fail(x, DVI_ERR_ARG, "opt_step must be >= 1");
+// What the AdamW step needs of an update's arguments (Adam's own take anything).
+static const char *check_adam(const dvi_ctx *x, float lr, float beta1, float beta2, float eps) {
+    if (!x->adamw || lr == 0.f) return nullptr;
+    if (!isfinite(lr)) return "lr must be finite";
+    if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f)) return "0 <= beta1, beta2 < 1";
+    if (!(eps > 0.f) || !isfinite(eps)) return "eps must be > 0";
+    return nullptr;
+}
+
+// What both updates take from the context.
+static UpdateArgs update_args(const dvi_ctx *x) {
     const dvi_config &cf = x->cfg;
-    const int n = x->ring_valid_h;
-    if (stats) memset(stats, 0, sizeof(*stats));
-    if (n == 0) return DVI_OK;
-    ev_begin(x, 3);
     UpdateArgs u{};
     u.W = x->head;
     u.Hh = x->ring_h;
@@ -1259,17 +1269,11 @@ extern "C" dvi_status dvi_update_drafter(dvi_ctx *x, const dvi_update_args *ua, 
     u.a = x->ring_a;
     u.r = x->ring_r;
     u.fresh = x->ring_fresh;
-    u.n = n;
+    u.n = x->ring_valid_h;
     u.V = cf.vocab;
     u.d = cf.d_model;
     u.rank = cf.lora_rank;
     u.gamma = cf.lora_gamma;
-    u.tau = ua->tau;
-    u.baseline = ua->baseline;
-    u.c_kl = ua->c_kl;
-    u.c_ce = ua->c_ce;
-    u.c_pg = ua->c_pg;
-    u.c_ent = ua->c_ent;
     u.A = x->lora_A;
     u.Bm = x->lora_B;
     u.u = x->upd_u;
@@ -1281,18 +1285,29 @@ extern "C" dvi_status dvi_update_drafter(dvi_ctx *x, const dvi_update_args *ua, 
     u.dB = x->upd_dB;
     u.loss_out = x->upd_loss;
     u.xfm = x->ufm;
-    launch_update_forward(x->dt, u, x->stream);
-    launch_update_backward(x->dt, u, x->stream);
+    return u;
+}
+
+static AdamArgs adam_numbers(double lr, double beta1, double beta2, double eps, double decay, int32_t step, double max_norm,
+                             uint64_t seed);
+static void launch_adam_step(DType pt, bool master, DType gt, int bits, const dvi_adamw_tensor *tensors, int n_tensors,
+                             AdamArgs a, double *part, float *norm, hipStream_t s);
+
+// The end of both updates: gradients to the caller, the optimizer's step, fresh rows' log-probabilities
+// (logp[i * stride]) kept and their flags cleared.
+static dvi_status update_end(dvi_ctx *x, float *grad_A_out, float *grad_B_out, float lr, float beta1, float beta2, float eps,
+                             int32_t opt_step, const float *logp, int stride) {
+    const dvi_config &cf = x->cfg;
     const size_t nA = (size_t)cf.vocab * cf.lora_rank, nB = (size_t)cf.lora_rank * cf.d_model;
     FinishArgs f{};
     f.gA = x->upd_dA;
     f.gB = x->upd_dB;
-    f.outA = own_memory(x, ua->grad_A_out) ? ua->grad_A_out : nullptr;
-    f.outB = own_memory(x, ua->grad_B_out) ? ua->grad_B_out : nullptr;
-    if (ua->grad_A_out && !f.outA)
-        HIPCHK(x, hipMemcpyAsync(ua->grad_A_out, x->upd_dA, nA * 4, hipMemcpyDeviceToDevice, x->stream));
-    if (ua->grad_B_out && !f.outB)
-        HIPCHK(x, hipMemcpyAsync(ua->grad_B_out, x->upd_dB, nB * 4, hipMemcpyDeviceToDevice, x->stream));
+    f.outA = own_memory(x, grad_A_out) ? grad_A_out : nullptr;
+    f.outB = own_memory(x, grad_B_out) ? grad_B_out : nullptr;
+    if (grad_A_out && !f.outA)
+        HIPCHK(x, hipMemcpyAsync(grad_A_out, x->upd_dA, nA * 4, hipMemcpyDeviceToDevice, x->stream));
+    if (grad_B_out && !f.outB)
+        HIPCHK(x, hipMemcpyAsync(grad_B_out, x->upd_dB, nB * 4, hipMemcpyDeviceToDevice, x->stream));
     f.A = x->lora_A;
     f.B = x->lora_B;
     f.mA = x->mA;
@@ -1303,11 +1318,56 @@ extern "C" dvi_status dvi_update_drafter(dvi_ctx *x, const dvi_update_args *ua, 
     f.nB = (long)nB;
     f.fresh = x->ring_fresh;
     f.ring_rows = cf.buffer_rows;
-    f.lr = ua->lr;
-    f.b1 = ua->beta1;
-    f.b2 = ua->beta2;
-    f.eps = ua->eps;
-    launch_update_finish(f, ua->opt_step, x->stream);
+    f.logp = logp;
+    f.logp_stride = stride;
+    f.n = x->ring_valid_h;
+    f.old = x->ring_old;
+    f.lr = x->adamw ? 0.f : lr;
+    f.b1 = beta1;
+    f.b2 = beta2;
+    f.eps = eps;
+    launch_update_finish(f, opt_step, x->stream);
+    if (x->adamw && lr != 0.f) {
+        // 8-bit codes lie at the start of the fp32 moments' buffers, their scales behind them (n codes and n / 64
+        // bytes of scales; n is a multiple of 16)
+        dvi_adamw_tensor t[2] = {{(int64_t)nA, x->lora_A, nullptr, x->upd_dA, x->mA, x->vA, nullptr, nullptr},
+                                 {(int64_t)nB, x->lora_B, nullptr, x->upd_dB, x->mB, x->vB, nullptr, nullptr}};
+        if (x->opt.state_bits == 8)
+            for (dvi_adamw_tensor &e : t) {
+                e.m_scale = (float *)((uint8_t *)e.m + e.n);
+                e.v_scale = (float *)((uint8_t *)e.v + e.n);
+            }
+        launch_adam_step(DType::F32, false, DType::F32, x->opt.state_bits, t, 2,
+                         adam_numbers(lr, beta1, beta2, eps, x->opt.weight_decay, opt_step, x->opt.max_norm, x->opt.seed),
+                         (double *)x->op_ws, nullptr, x->stream);
+    }
+    return DVI_OK;
+}
+
+extern "C" dvi_status dvi_update_drafter(dvi_ctx *x, const dvi_update_args *ua, dvi_update_stats *stats) {
+    if (!x || !ua) return DVI_ERR_ARG;
+    if (x->device_error) return fail(x, DVI_ERR_DEVICE, "context has a sticky device error");
+    if (x->state != S_READY) return fail(x, DVI_ERR_STATE, "update needs state READY");
+    if (!(ua->tau > 0.f)) return fail(x, DVI_ERR_ARG, "tau must be > 0");
+    if (ua->lr != 0.f && ua->opt_step < 1) return fail(x, DVI_ERR_ARG, "opt_step must be >= 1");
+    const char *bad = check_adam(x, ua->lr, ua->beta1, ua->beta2, ua->eps);
+    if (bad) return fail(x, DVI_ERR_ARG, "%s", bad);
+    if (stats) memset(stats, 0, sizeof(*stats));
+    if (x->ring_valid_h == 0) return DVI_OK;
+    ev_begin(x, 3);
+    UpdateArgs u = update_args(x);
+    u.tau = ua->tau;
+    u.baseline = ua->baseline;
+    u.c_kl = ua->c_kl;
+    u.c_ce = ua->c_ce;
+    u.c_pg = ua->c_pg;
+    u.c_ent = ua->c_ent;
+    launch_update_logits(x->dt, u, x->stream);
+    launch_update_rows(u, x->stream);
+    launch_update_backward(x->dt, u, x->stream);
+    const dvi_status end = update_end(x, ua->grad_A_out, ua->grad_B_out, ua->lr, ua->beta1, ua->beta2, ua->eps, ua->opt_step,
+                                      x->upd_stats + 2, 8);
+    if (end != DVI_OK) return end;
     ev_end(x, 3);
     LAUNCHCHK(x);
     float lo[16];
@@ -1324,6 +1384,90 @@ extern "C" dvi_status dvi_update_drafter(dvi_ctx *x, const dvi_update_args *ua, 
         stats->fresh = (int32_t)lo[7];
         stats->fresh_accepted = (int32_t)lo[8];
     }
+    return DVI_OK;
+}
+
+extern "C" dvi_status dvi_update_policy(dvi_ctx *x, const dvi_policy_update_args *ua, dvi_policy_update_stats *stats) {
+    if (!x || !ua) return DVI_ERR_ARG;
+    if (x->device_error) return fail(x, DVI_ERR_DEVICE, "context has a sticky device error");
+    if (x->state != S_READY) return fail(x, DVI_ERR_STATE, "update needs state READY");
+    if (!(ua->tau >= 1e-6f && ua->tau <= 1e6f)) return fail(x, DVI_ERR_ARG, "tau must be from 1e-6 to 1e6");
+    if (!(ua->clip_low >= 0.f && ua->clip_low <= 1.f) || !(ua->clip_high >= 0.f))
+        return fail(x, DVI_ERR_ARG, "0 <= clip_low <= 1 and 0 <= clip_high");
+    if (!isfinite(ua->c_pg) || !isfinite(ua->c_kl) || !isfinite(ua->c_ent) || !isfinite(ua->baseline))
+        return fail(x, DVI_ERR_ARG, "coefficients and baseline must be finite");
+    if (ua->lr != 0.f && ua->opt_step < 1) return fail(x, DVI_ERR_ARG, "opt_step must be >= 1");
+    const char *bad = check_adam(x, ua->lr, ua->beta1, ua->beta2, ua->eps);
+    if (bad) return fail(x, DVI_ERR_ARG, "%s", bad);
+    if (stats) memset(stats, 0, sizeof(*stats));
+    const int n = x->ring_valid_h;
+    if (n == 0) return DVI_OK;
+    ev_begin(x, 3);
+    const UpdateArgs u = update_args(x);
+    launch_update_logits(x->dt, u, x->stream);
+    RowArgs a{};
+    a.z = a.dz = u.Z;  // the gradient takes the logits' place, where the LoRA gradients' kernels read it
+    a.ldz = a.lddz = a.ldq = u.V;
+    a.q = u.logits;
+    a.tok = u.a;
+    a.N = n;
+    a.V = u.V;
+    a.it = 1.0;
+    a.iq = 1.0 / (double)ua->tau;
+    a.logp = x->pol_logp;
+    a.policy = 1;
+    a.old = x->ring_old;
+    a.on_policy = u.fresh;
+    a.reward = u.r;
+    a.reward_scale = ua->c_pg;
+    a.baseline = ua->baseline;
+    a.w0 = (float)(1.0 / n);
+    a.lo = 1.0 - (double)ua->clip_low;
+    a.hi = 1.0 + (double)ua->clip_high;
+    a.c_kl = ua->c_kl;
+    a.c_ent = ua->c_ent;
+    a.terms = x->pol_terms;
+    launch_rows(DType::F32, a, x->op_ws, x->stream);
+    launch_update_backward(x->dt, u, x->stream);
+    const dvi_status end = update_end(x, ua->grad_A_out, ua->grad_B_out, ua->lr, ua->beta1, ua->beta2, ua->eps, ua->opt_step,
+                                      x->pol_logp, 1);
+    if (end != DVI_OK) return end;
+    ev_end(x, 3);
+    LAUNCHCHK(x);
+    float te[5], counts[4];
+    HIPCHK(x, hipMemcpyAsync(te, x->pol_terms, sizeof(te), hipMemcpyDeviceToHost, x->stream));
+    HIPCHK(x, hipMemcpyAsync(counts, x->upd_loss + 12, sizeof(counts), hipMemcpyDeviceToHost, x->stream));
+    HIPCHK(x, hipStreamSynchronize(x->stream));
+    if (stats) {
+        stats->loss = te[0];
+        stats->policy = te[1];
+        stats->kl = te[2];
+        stats->entropy = te[3];
+        stats->clipped = te[4];
+        stats->rows = (int32_t)counts[0];
+        stats->accepted = (int32_t)counts[1];
+        stats->fresh = (int32_t)counts[2];
+        stats->fresh_accepted = (int32_t)counts[3];
+    }
+    return DVI_OK;
+}
+
+extern "C" dvi_status dvi_set_optimizer(dvi_ctx *x, const dvi_optimizer *opt) {
+    if (!x) return DVI_ERR_ARG;
+    if (x->device_error) return fail(x, DVI_ERR_DEVICE, "context has a sticky device error");
+    if (x->state == S_DRAFTED || x->state == S_VERIFIED) return fail(x, DVI_ERR_STATE, "set_optimizer during a step");
+    if (opt) {
+        if (opt->state_bits != 8 && opt->state_bits != 32) return fail(x, DVI_ERR_ARG, "state_bits must be 8 or 32");
+        if (!isfinite(opt->weight_decay)) return fail(x, DVI_ERR_ARG, "weight_decay must be finite");
+        if (!(opt->max_norm >= 0.0)) return fail(x, DVI_ERR_ARG, "max_norm must not be negative");
+    }
+    const dvi_config &cf = x->cfg;
+    const int nA = cf.vocab * cf.lora_rank, nB = cf.lora_rank * cf.d_model;
+    for (float *p : {x->mA, x->vA}) fill_i32_kernel<<<(nA + 255) / 256, 256, 0, x->stream>>>((int32_t *)p, nA, 0);
+    for (float *p : {x->mB, x->vB}) fill_i32_kernel<<<(nB + 255) / 256, 256, 0, x->stream>>>((int32_t *)p, nB, 0);
+    LAUNCHCHK(x);
+    x->adamw = opt != nullptr;
+    if (opt) x->opt = *opt;
     return DVI_OK;
 }
 
@@ -1712,7 +1856,8 @@ extern "C" dvi_status dvi_write_buffer(dvi_ctx *x, int32_t nrows, const float *h
             ((float *)tmp.data())[e] = h[e];
         }
     }
-    std::vector<int32_t> zi(nrows, 0), neg(nrows, -1);
+    std::vector<int32_t> zi(nrows, 0), neg(nrows, -1), nan(nrows, 0x7fc00000);
+    HIPCHK(x, hipMemcpy(x->ring_old, nan.data(), nrows * 4, hipMemcpyHostToDevice));  // not known for any of them
     HIPCHK(x, hipMemcpy(x->ring_h, tmp.data(), tmp.size(), hipMemcpyHostToDevice));
     HIPCHK(x, hipMemcpy(x->ring_logits, logits, (size_t)nrows * V * 4, hipMemcpyHostToDevice));
     HIPCHK(x, hipMemcpy(x->ring_a, a, nrows * 4, hipMemcpyHostToDevice));

@@ -285,9 +285,12 @@ struct UpdateArgs {
     float *dB;              // [r][d]
     float *loss_out;        // [16]: loss, kl, ce, pg, entropy, n, n_acc, n_fresh, n_fresh_acc | counts at [12..16)
 };
-void launch_update_forward(DType t, const UpdateArgs &u, hipStream_t s);
+// The drafter's logits Z of the ring rows (with u and the row counts), and Z turned into g.
+void launch_update_logits(DType t, const UpdateArgs &u, hipStream_t s);
+void launch_update_rows(const UpdateArgs &u, hipStream_t s);
 void launch_update_backward(DType t, const UpdateArgs &u, hipStream_t s);
-// The update's end: gradients out (outA, outB: may be null), Adam unless lr == 0, fresh flags cleared.
+// The update's end: gradients out (outA, outB: may be null), Adam unless lr == 0, fresh flags cleared; the
+// rows that were fresh, or have none (NaN), keep their log-probability (logp[i * logp_stride], i < n) in old.
 struct FinishArgs {
     const float *gA, *gB;   // gradients [nA], [nB]
     float *outA, *outB;
@@ -295,6 +298,9 @@ struct FinishArgs {
     long nA, nB;
     int8_t *fresh;          // [ring_rows]
     int ring_rows;
+    const float *logp;
+    int logp_stride, n;
+    float *old;             // [ring_rows]
     float lr, b1, b2, eps, c1, c2;  // c1, c2: bias corrections, from the step number
 };
 void launch_update_finish(FinishArgs f, int step, hipStream_t s);

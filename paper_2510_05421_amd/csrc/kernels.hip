@@ -1633,7 +1633,7 @@ __global__ void __launch_bounds__(512) upd_dB_kernel(UpdateArgs u, int c0) {
     }
 }
 
-void launch_update_forward(DType t, const UpdateArgs &u, hipStream_t s) {
+void launch_update_logits(DType t, const UpdateArgs &u, hipStream_t s) {
     float *counts = u.loss_out + 12;
     const int prep = u.n * (u.rank + 1) + 1;
     if (t == DType::BF16)
@@ -1652,6 +1652,10 @@ void launch_update_forward(DType t, const UpdateArgs &u, hipStream_t s) {
     g.r = u.rank;
     g.gamma = u.gamma;
     launch_gemm_rows(t, EPI_LOGITS, g, s);
+}
+
+void launch_update_rows(const UpdateArgs &u, hipStream_t s) {
+    const float *counts = u.loss_out + 12;
     if (u.V <= 4096)
         upd_rows_kernel<4><<<u.n, 1024, 0, s>>>(u, counts);
     else
@@ -1674,14 +1678,17 @@ void launch_update_backward(DType t, const UpdateArgs &u, hipStream_t s) {
 
 // The end of an update in one launch (as two Adam launches, two gradient copies and the flag reset:
 // 20 us of launches for 4 us of memory traffic): thread i takes element i of A_s, then of B_s, then
-// clears ring flag i - nA - nB.
+// keeps the log-probability of ring row i - nA - nB, if it was fresh or has none, and clears its flag.
 __global__ void __launch_bounds__(256) upd_finish_kernel(FinishArgs f) {
     long i = (long)blockIdx.x * 256 + threadIdx.x;
     const bool isA = i < f.nA;
     if (!isA) i -= f.nA;
     if (!isA && i >= f.nB) {
         i -= f.nB;
-        if (i < f.ring_rows) f.fresh[i] = 0;
+        if (i < f.ring_rows) {
+            if (i < f.n && (f.fresh[i] != 0 || isnan(f.old[i]))) f.old[i] = f.logp[i * f.logp_stride];
+            f.fresh[i] = 0;
+        }
         return;
     }
     const float gi = (isA ? f.gA : f.gB)[i];

@@ -30,7 +30,9 @@ struct RowArgs {
     // policy loss (policy != 0)
     int policy;
     const float *adv, *old, *weights, *ref_logp;  // [N]; old, weights, ref_logp may be nullptr
-    const int8_t *on_policy; // [N] or nullptr: rows whose ratio is 1
+    const int8_t *on_policy; // [N] or nullptr: rows whose ratio is 1; with it a NaN in old says the same
+    const int8_t *reward;    // [N] or nullptr: advantages reward_scale (reward - baseline) instead of adv
+    float reward_scale, baseline;
     float w0;                // weight of every row where weights == nullptr
     double lo, hi;           // 1 - clip_low, 1 + clip_high
     double c_kl, c_ent;

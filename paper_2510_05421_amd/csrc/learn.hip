@@ -114,10 +114,10 @@ __device__ __forceinline__ RowIn row_in(const RowArgs &a, long i) {
     RowIn r = {a.tok[i], 1.f, 0.f, 0.f, 0.f, true, false};
     if (a.policy) {
         r.w = a.weights != nullptr ? a.weights[i] : a.w0;
-        r.adv = a.adv[i];
+        r.adv = a.reward != nullptr ? a.reward_scale * ((float)a.reward[i] - a.baseline) : a.adv[i];
         if (a.old != nullptr) {
             r.old = a.old[i];
-            r.on = a.on_policy != nullptr && a.on_policy[i] != 0;
+            r.on = a.on_policy != nullptr && (a.on_policy[i] != 0 || isnan(r.old));
         }
         if (a.ref_logp != nullptr) r.ref = a.ref_logp[i];
     }

@@ -245,6 +245,33 @@ class Engine:
             out["grad_A"], out["grad_B"] = g_A, g_B
         return out
 
+    def update_policy(self, c_pg=1.0, c_kl=0.0, c_ent=0.0, clip_low=0.2, clip_high=0.2, tau=1.0, baseline=0.0, lr=1e-3,
+                      beta1=0.9, beta2=0.999, eps=1e-8, opt_step=None, grads: bool = False):
+        """Clipped policy update over all replay rows (see dvi_update_policy); shares update_drafter's step count."""
+        g_A = torch.empty_like(self.lora_A) if grads else None
+        g_B = torch.empty_like(self.lora_B) if grads else None
+        if grads:
+            self.stream.wait_stream(torch.cuda.current_stream(self.device))
+        step = self.opt_step + 1 if opt_step is None and lr != 0.0 else int(opt_step or 0)
+        args = _abi.PolicyUpdateArgs(c_pg, c_kl, c_ent, clip_low, clip_high, tau, baseline, lr, beta1, beta2, eps, step,
+                                     _p(g_A), _p(g_B))
+        stats = _abi.PolicyUpdateStats()
+        self._check(self.lib.dvi_update_policy(self.ctx, ctypes.byref(args), ctypes.byref(stats)))
+        if opt_step is None:
+            self.opt_step = max(self.opt_step, step)
+        out = {k: getattr(stats, k) for k, _ in _abi.PolicyUpdateStats._fields_}
+        if grads:
+            out["grad_A"], out["grad_B"] = g_A, g_B
+        return out
+
+    def set_optimizer(self, state_bits: Optional[int] = None, weight_decay: float = 0.0, max_norm: float = 0.0, seed: int = 0):
+        """AdamW with 32- or 8-bit states for both updates (see dvi_set_optimizer), or with state_bits None the
+        plain Adam they start with.  Clears the moments and the step count."""
+        opt = None if state_bits is None else ctypes.byref(
+            _abi.Optimizer(state_bits, weight_decay, max_norm, int(seed) & 0xFFFFFFFFFFFFFFFF))
+        self._check(self.lib.dvi_set_optimizer(self.ctx, opt))
+        self.opt_step = 0
+
     # ------------------------------------------------------------------ inspection
     def read_kv(self, layer: int, seq: int, pos0: int, npos: int):
         c = self.cfg
@@ -316,12 +343,14 @@ class Engine:
 
     # ------------------------------------------------------------------ driver
     def generate(self, prompts, n_new: int, k_spec: int, update_every: int = 0,
-                 schedule: Optional[KLRLSchedule] = None, lr: float = 1e-3, on_step=None, lens=None):
+                 schedule: Optional[KLRLSchedule] = None, lr: float = 1e-3, on_step=None, lens=None, clip=None):
         """Prefill then decode until every sequence has n_new tokens (the first from the prefill).
 
         Returns (tokens [B, n_new], info) with per-step accept lengths m and commit counts n.
         update_every > 0 runs a drafter update after every update_every decode steps, with
-        coefficients from the KL->RL schedule.  lens: per-sequence prompt lengths (see prefill)."""
+        coefficients from the KL->RL schedule.  clip = (low, high): clipped policy updates (update_policy,
+        with the schedule's KL, policy and entropy weights) instead.  lens: per-sequence prompt lengths (see
+        prefill)."""
         first = self.prefill(prompts, lens)
         B = self.batch
         out: List[List[int]] = [[int(t)] for t in first]
@@ -343,8 +372,11 @@ class Engine:
                 on_step(self, step)
             if update_every and step % update_every == 0 and k_spec > 1:
                 c = sched.coeffs(self.updates, self.baseline)
-                st = self.update_drafter(c["c_kl"], c["c_ce"], c["c_pg"], c["c_ent"], c["tau"],
-                                         self.baseline, lr=lr)
+                if clip is not None:
+                    st = self.update_policy(c["c_pg"], c["c_kl"], c["c_ent"], clip[0], clip[1], c["tau"], self.baseline, lr=lr)
+                else:
+                    st = self.update_drafter(c["c_kl"], c["c_ce"], c["c_pg"], c["c_ent"], c["tau"],
+                                             self.baseline, lr=lr)
                 upd.append(st)
                 if st["fresh"] > 0:
                     self.baseline = sched.ema(self.baseline, st["fresh_accepted"] / st["fresh"])

@@ -1,0 +1,230 @@
+"""The clipped policy update of the drafter, and both updates under AdamW, against 64 bits.
+
+The reference takes the drafter's logits from the oracle (float64) and writes the loss out.  Gradients are
+held to 1e-4 of their norm, as those of the drafter update are (fp32 sums over d and the vocabulary, in
+bf16 storage of exactly representable states and weights); parameters of one optimizer step are held to
+the step from the gradients that came back.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+
+import gpu_util as gu
+import oracle.update as ou
+import synth
+
+pytestmark = pytest.mark.gpu
+
+TINY = synth.TINY.replace(name="policy", n_layers=1, split_k=1, d_model=64, n_heads=1, n_kv_heads=1, head_dim=64, ffn_dim=32,
+                          vocab=1008, lora_rank=8)
+
+
+def policy(W, A, B, gamma, h, a, q_logits, r, old, c_pg, c_kl, c_ent, lo, hi, tau, baseline):
+    """Loss terms, gradients of both factors and the rows' log-probabilities in 64 bits; old: NaN where the row
+    is at its first update."""
+    z, u = ou.draft_logits(W, A, B, gamma, h)
+    n = z.shape[0]
+    logp = ou.log_softmax(z)
+    p = np.exp(logp)
+    logq = ou.log_softmax(np.asarray(q_logits, np.float64) / tau)
+    kl = (p * (logp - logq)).sum(1)
+    ent = -(p * logp).sum(1)
+    lpa = logp[np.arange(n), a]
+    ratio = np.exp(lpa - np.where(np.isnan(old), lpa, old))
+    adv = c_pg * (r.astype(np.float64) - baseline)
+    held = np.clip(ratio, 1 - lo, 1 + hi) * adv
+    cut = held < ratio * adv
+    pol = -np.where(cut, held, ratio * adv)
+    by = np.where(cut, 0.0, -ratio * adv)
+    hot = np.zeros_like(p)
+    hot[np.arange(n), a] = 1.0
+    g = (by[:, None] * (hot - p) + c_kl * p * (logp - logq - kl[:, None]) + c_ent * p * (logp + ent[:, None])) / n
+    dA = gamma * (g.T @ u)
+    dB = (gamma * (g @ A)).T @ h
+    loss = (pol + c_kl * kl - c_ent * ent).mean()
+    return dict(loss=loss, policy=pol.mean(), kl=kl.mean(), entropy=ent.mean(), clipped=cut.mean()), dA, dB, lpa
+
+
+def setup(shape, rows, seed=11, buffer_rows=256):
+    w = synth.make_weights(shape, 0, lora_A_std=0.3)
+    eng, _ = gu.engine(shape, max_seq=64, weights=w, buffer_rows=buffer_rows)
+    eng.prefill(synth.make_prompts(shape.vocab, 1, 4, 1))
+    buf = synth.make_buffer(shape.d_model, shape.vocab, rows, seed=seed)
+    if rows:
+        eng.write_buffer(buf.h, buf.a, buf.logits, buf.r, buf.fresh)
+    W = w.as_f32(w.lm_head).astype(np.float64)
+    return eng, buf, W
+
+
+def factors(eng):
+    return eng.lora_A.cpu().numpy().astype(np.float64), eng.lora_B.cpu().numpy().astype(np.float64)
+
+
+COEF = dict(c_pg=1.5, c_kl=0.4, c_ent=0.02, clip_low=0.2, clip_high=0.28, tau=1.3, baseline=0.35)
+
+
+def ref(W, A, B, shape, buf, old, k=None):
+    c = dict(COEF, **(k or {}))
+    return policy(W, A, B, shape.lora_gamma, buf.h, buf.a, buf.logits, buf.r, old, c["c_pg"], c["c_kl"], c["c_ent"],
+                  c["clip_low"], c["clip_high"], c["tau"], c["baseline"])
+
+
+def check(st, want, terms=True):
+    t, dA, dB, _ = want
+    assert gu.rel_l2(st["grad_A"].cpu().numpy(), dA) <= 1e-4
+    assert gu.rel_l2(st["grad_B"].cpu().numpy(), dB) <= 1e-4
+    for k, v in t.items():
+        assert abs(st[k] - v) <= 1e-5 * (1 + abs(t["entropy"])), (k, st[k], v)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("rows,vocab,rank", [(1, 1008, 8), (7, 16, 1), (48, 1008, 8), (255, 4112, 20), (16, 33024, 16),
+                                             (4, 65552, 4)])
+def test_updates_reuse_the_rows(rows, vocab, rank, bf16):
+    """Four updates over the same rows: the first at ratio 1, the next against the log-probabilities it kept,
+    with steps large enough that some ratios are clipped."""
+    shape = TINY.replace(vocab=vocab, lora_rank=rank, bf16=bf16)
+    eng, buf, W = setup(shape, rows)
+    old = np.full(rows, np.nan)
+    clipped = 0.0
+    for k in range(4):
+        A, B = factors(eng)
+        st = eng.update_policy(**COEF, lr=0.05, grads=True)
+        want = ref(W, A, B, shape, buf, old)
+        # a ratio within fp32's reach of a border (its logits carry about 1e-6) may fall on either side
+        ratio = np.exp(want[3] - np.where(np.isnan(old), want[3], old))
+        assert (np.abs(ratio - 0.8) > 1e-4).all() and (np.abs(ratio - 1.28) > 1e-4).all()
+        check(st, want)
+        assert st["rows"] == rows and st["accepted"] == int(buf.r.sum())
+        assert st["fresh"] == (int(buf.fresh.sum()) if k == 0 else 0)
+        if k == 0:
+            old = want[3]
+            assert st["clipped"] == 0.0
+        clipped += st["clipped"]
+    assert rows < 40 or clipped > 0
+    eng.close()
+
+
+def test_rows_that_another_update_used_keep_their_log_probabilities():
+    """The drafter update clears the fresh flags and keeps what the policy update needs."""
+    shape = TINY
+    eng, buf, W = setup(shape, 40)
+    A0, B0 = factors(eng)
+    eng.update_drafter(0.7, 0.9, 0.4, 0.05, 1.3, 0.35, lr=0.05)
+    _, _, _, old = ref(W, A0, B0, shape, buf, np.full(40, np.nan))
+    A, B = factors(eng)
+    st = eng.update_policy(**COEF, lr=0.0, grads=True)
+    check(st, ref(W, A, B, shape, buf, old))
+    assert st["fresh"] == 0
+    eng.close()
+
+
+def test_a_decode_loop_trains_by_the_policy_update():
+    """Rows logged by decoding; a slot of the ring that is logged anew is fresh again."""
+    shape = synth.TINY
+    eng, _ = gu.engine(shape, max_batch=2, max_seq=200, buffer_rows=24, lora_A_std=0.05)
+    eng.set_optimizer(8, weight_decay=0.01, max_norm=1.0, seed=3)
+    prompts = synth.make_prompts(shape.vocab, 2, 12, 5)
+    plain, _ = eng.generate(prompts, 40, 4)
+    eng.opt_step = 0
+    toks, info = eng.generate(prompts, 40, 4, update_every=3, clip=(0.2, 0.28), lr=1e-3)
+    assert np.array_equal(toks, plain)          # decoding stays greedy decoding, whatever the drafter learns
+    assert len(info["updates"]) >= 3
+    for u in info["updates"]:
+        assert np.isfinite([u[k] for k in ("loss", "policy", "kl", "entropy", "clipped")]).all() and u["rows"] > 0
+    assert info["updates"][-1]["rows"] == 24 and 0 < info["updates"][-1]["fresh"] < 24
+    A, B = factors(eng)
+    assert np.isfinite(A).all() and np.isfinite(B).all()
+    # the ring as it is: rows logged since the last update count at ratio 1
+    rows = eng.read_buffer(0, 24)
+    W = synth.make_weights(shape, 0, lora_A_std=0.05).lm_head.astype(np.float64)
+    rows["old"] = np.where(rows["fresh"] != 0, np.nan, 0.0)
+    st = eng.update_policy(**COEF, lr=0.0, grads=True)
+    st2 = eng.update_policy(**COEF, lr=0.0, grads=True)
+    assert st["fresh"] == int(rows["fresh"].sum()) and st2["fresh"] == 0
+    # nothing moved in between: fresh rows have ratio 1 in both
+    assert np.allclose(st["grad_A"].cpu().numpy(), st2["grad_A"].cpu().numpy(), rtol=1e-5, atol=1e-9)
+    eng.close()
+
+
+def adamw_step(p, g, m, v, t, lr, wd, clip):
+    g = g * clip
+    m, v = 0.9 * m + 0.1 * g, 0.999 * v + 0.001 * g * g
+    return p - lr * wd * p - lr * (m / (1 - 0.9 ** t)) / (np.sqrt(v / (1 - 0.999 ** t)) + 1e-8), m, v
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("which", ["policy", "drafter"])
+@pytest.mark.parametrize("max_norm", [0.0, 0.01])
+def test_both_updates_step_by_adamw(which, bits, max_norm):
+    """Parameters against the step from the gradients that the update returned: float arguments are 2^-25 off
+    what they stand for, which 1 - beta2 shows as 2.4e-5 of itself and sqrt(v) as half of that."""
+    eng, buf, W = setup(TINY, 60)
+    lr, wd = 1e-2, 0.1
+    eng.set_optimizer(bits, weight_decay=wd, max_norm=max_norm, seed=7)
+    m, v = [0.0, 0.0], [0.0, 0.0]
+    for t in range(1, 4 if bits == 32 else 2):
+        p = factors(eng)
+        if which == "policy":
+            st = eng.update_policy(**COEF, lr=lr, grads=True)
+        else:
+            eng.write_buffer(buf.h, buf.a, buf.logits, buf.r, buf.fresh)
+            st = eng.update_drafter(0.7, 0.9, 0.4, 0.05, 1.3, 0.35, lr=lr, grads=True)
+        g = [st[k].cpu().numpy().astype(np.float64) for k in ("grad_A", "grad_B")]
+        norm = np.sqrt(sum((x * x).sum() for x in g))
+        clip = min(1.0, max_norm / norm) if max_norm else 1.0
+        assert max_norm == 0.0 or clip < 1.0
+        now = factors(eng)
+        for k in range(2):
+            want, m[k], v[k] = adamw_step(p[k], g[k], m[k], v[k], t, lr, wd, clip)
+            assert np.abs(now[k] - want).max() <= 5e-5 * lr * 4 + 2.0 ** -22 * np.abs(want).max()
+    eng.close()
+
+
+def test_the_default_optimizer_is_as_it_was_and_comes_back():
+    eng, buf, W = setup(TINY, 30)
+    eng2, _, _ = setup(TINY, 30)
+    eng.set_optimizer(8, max_norm=1.0)
+    eng.update_policy(**COEF, lr=1e-3)
+    eng.set_optimizer(None)                       # Adam, its moments cleared
+    for e in (eng, eng2):
+        e.write_buffer(buf.h, buf.a, buf.logits, buf.r, buf.fresh)
+    eng.lora_A.copy_(eng2.lora_A)
+    eng.lora_B.copy_(eng2.lora_B)
+    import torch
+    torch.cuda.synchronize()
+    for _ in range(3):
+        a = eng.update_drafter(0.7, 0.9, 0.4, lr=1e-3)
+        b = eng2.update_drafter(0.7, 0.9, 0.4, lr=1e-3)
+        assert a == b
+    assert torch.equal(eng.lora_A, eng2.lora_A) and torch.equal(eng.lora_B, eng2.lora_B)
+    eng.close()
+    eng2.close()
+
+
+def test_refusals():
+    from paper_2510_05421_amd import _abi
+    eng, buf, W = setup(TINY, 0)
+    assert eng.update_policy(**COEF)["rows"] == 0     # an empty ring: nothing to do
+    for kw in (dict(tau=0.0), dict(tau=float("nan")), dict(clip_low=1.5), dict(clip_low=-0.1), dict(clip_high=-1.0),
+               dict(c_pg=float("inf")), dict(c_kl=float("nan")), dict(baseline=float("nan")), dict(opt_step=0)):
+        with pytest.raises(_abi.DVIError) as e:
+            eng.update_policy(**dict(COEF, **kw))
+        assert e.value.status == _abi.ERR_ARG
+    for kw in (dict(state_bits=16), dict(state_bits=8, max_norm=-1.0), dict(state_bits=8, max_norm=float("nan")),
+               dict(state_bits=32, weight_decay=float("inf"))):
+        with pytest.raises(_abi.DVIError) as e:
+            eng.set_optimizer(**kw)
+        assert e.value.status == _abi.ERR_ARG
+    eng.set_optimizer(32)
+    with pytest.raises(_abi.DVIError):
+        eng.update_policy(**COEF, beta2=1.0)
+    eng.draft(4)
+    for call in (lambda: eng.update_policy(**COEF), lambda: eng.set_optimizer(32)):
+        with pytest.raises(_abi.DVIError) as e:
+            call()
+        assert e.value.status == _abi.ERR_STATE
+    eng.abort()
+    assert eng.lib.dvi_update_policy(eng.ctx, None, None) == _abi.ERR_ARG
+    eng.close()

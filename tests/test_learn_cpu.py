@@ -84,6 +84,8 @@ def test_adamw_refuses(tensor, kw):
 
 def test_null_arguments_are_refused():
     lib = _abi.load()
+    assert lib.dvi_update_policy(None, None, None) == _abi.ERR_ARG
+    assert lib.dvi_set_optimizer(None, None) == _abi.ERR_ARG
     t, args = _adamw()
     assert lib.dvi_token_logprobs(None, A, 1 << 20, None) == _abi.ERR_ARG
     assert lib.dvi_policy_loss(None, A, 1 << 20, None) == _abi.ERR_ARG
@@ -94,8 +96,9 @@ def test_null_arguments_are_refused():
 
 def test_capacity_and_workspaces():
     lib = _abi.load()
-    for name, args in (("dvi_token_logprobs", _logprob()), ("dvi_policy_loss", _policy())):
-        need = getattr(lib, name + "_workspace_bytes")(4, 100)
+    wide = dict(vocab=200000, ld=200000)     # split over workgroups: sums of the parts
+    for name, args in (("dvi_token_logprobs", _logprob(**wide)), ("dvi_policy_loss", _policy(grad_ld=200000, grad=1 << 40, **wide))):
+        need = getattr(lib, name + "_workspace_bytes")(4, 200000)
         assert 0 < need < 1 << 20
         assert getattr(lib, name)(args, A, need - 1, None) == _abi.ERR_CAPACITY
         assert getattr(lib, name)(args, A + 128, need, None) == _abi.ERR_ARG      # not aligned
@@ -127,7 +130,8 @@ def test_argument_structures_have_the_headers_layout(tmp_path):
     import os
     import subprocess
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    pairs = [("dvi_logprob_args", _abi.LogprobArgs), ("dvi_policy_args", _abi.PolicyArgs),
+    pairs = [("dvi_policy_update_args", _abi.PolicyUpdateArgs), ("dvi_policy_update_stats", _abi.PolicyUpdateStats),
+             ("dvi_optimizer", _abi.Optimizer), ("dvi_logprob_args", _abi.LogprobArgs), ("dvi_policy_args", _abi.PolicyArgs),
              ("dvi_adamw_tensor", _abi.AdamwTensor), ("dvi_adamw_args", _abi.AdamwArgs)]
     lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "dvi.h"', "int main(void) {"]
     for c, py in pairs:
