@@ -757,11 +757,8 @@ size_t rows_workspace(long N, int V, bool policy) {
 template <DType T, bool REF, int NT, int NC, int SL = 0, bool BIG = false>
 static void launch_row_shape(const RowArgs &a, hipStream_t s) {
     constexpr int lds = SL * (REF ? 2 : 1) * NT * 16;
-    if (lds > 0) {
-        static const hipError_t set = hipFuncSetAttribute((const void *)row_kernel<T, REF, NT, NC, SL, BIG>,
-                                                          hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        (void)set;
-    }
+    if (lds > 0)  // for the current device, each time; a refusal shows at the launch
+        (void)hipFuncSetAttribute((const void *)row_kernel<T, REF, NT, NC, SL, BIG>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     row_kernel<T, REF, NT, NC, SL, BIG><<<(unsigned)a.N, NT, lds, s>>>(a);
 }
 
@@ -1101,7 +1098,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamTable tab, AdamArgs a) {
             mm = wave_max(mm);
             rm = wave_max(rm);
             constexpr float kTiny = 0x1p-100f;  // blocks whose largest is below are held as zeros
-            const float im = mm < kTiny ? 0.f : 448.f / mm, ir = rm < kTiny ? 0.f : 448.f / rm;
+            const float im = mm < kTiny ? 0.f : 1.f / mm * 448.f, ir = rm < kTiny ? 0.f : 1.f / rm * 448.f;
             float mc[4], rc[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -1117,8 +1114,8 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamTable tab, AdamArgs a) {
             store4_codes<ONCE>(t.m, i, n, (uint32_t)mw);
             store4_codes<ONCE>(t.v, i, n, (uint32_t)rw);
             if (lane == 0) {
-                t.ms[i / kStateBlock] = mm < kTiny ? 0.f : mm / 448.f;
-                t.vs[i / kStateBlock] = rm < kTiny ? 0.f : rm / 448.f;
+                t.ms[i / kStateBlock] = mm < kTiny ? 0.f : mm * (1.f / 448.f);
+                t.vs[i / kStateBlock] = rm < kTiny ? 0.f : rm * (1.f / 448.f);
             }
         }
     }
