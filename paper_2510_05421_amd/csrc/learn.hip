@@ -192,9 +192,15 @@ struct Scale {
 };
 __device__ __forceinline__ Scale scale_of(float M, float k) {
 #pragma clang fp contract(off)  // b is the rounded product wherever it goes
-    const float two = __uint_as_float(__float_as_uint(k) & 0x7f800000u), p = fabsf(M * k);
-    k = p < 0x1p31f ? k : p < 0x1p100f ? two : two * 0x1p-60f;
-    return {k, M * k};
+    Scale s = {k, M * k};
+    const bool large = !(fabsf(s.b) < 0x1p31f);
+    if (__builtin_amdgcn_ballot_w64(large) != 0) {  // hardly ever: a branch, not its instructions
+        const float two = __uint_as_float(__float_as_uint(k) & 0x7f800000u);
+        const float kl = fabsf(s.b) < 0x1p100f ? two : two * 0x1p-60f;
+        s.k = large ? kl : k;
+        s.b = large ? M * kl : s.b;
+    }
+    return s;
 }
 
 // The sums of one more chunk, x of the logits and y of the reference's: s = sum 2^x, t = sum 2^x x and, for the
@@ -220,20 +226,34 @@ __device__ __forceinline__ void add_chunk(RowStats &r, const uint4 &zc, const ui
     }
 }
 
+// A thread's sums and the scales that they are relative to.
+struct Sums {
+    RowStats r;
+    Scale z, q;
+};
+__device__ __forceinline__ Sums no_sums(float za, float kz, float kq) {
+    return {{kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, za, 0.f}, scale_of(kLowest, kz), scale_of(kLowest, kq)};
+}
+
 // Sums relative to new maxima M, Mq (at least the old ones).
 template <bool REF>
-__device__ __forceinline__ void rebase(RowStats &r, float M, float Mq, float kz, float kq) {
-    const float dx = scale_of(r.M, kz).b - scale_of(M, kz).b, f = __builtin_amdgcn_exp2f(dx);
+__device__ __forceinline__ void rebase(Sums &s, float M, float Mq, float kz, float kq) {
+    RowStats &r = s.r;
+    const Scale nz = scale_of(M, kz);
+    const float dx = s.z.b - nz.b, f = __builtin_amdgcn_exp2f(dx);
     if (REF) {
         // a reference masked by the lowest number: dy is as large as that, and counts only where f s does
-        const float dy = scale_of(r.Mq, kq).b - scale_of(Mq, kq).b;
+        const Scale nq = scale_of(Mq, kq);
+        const float dy = s.q.b - nq.b;
         r.k = mul0(f, r.k + mul0(r.s, dx - dy));
         r.sq *= __builtin_amdgcn_exp2f(dy);
         r.Mq = Mq;
+        s.q = nq;
     }
     r.t = mul0(f, r.t + mul0(r.s, dx));
     r.s *= f;
     r.M = M;
+    s.z = nz;
 }
 
 template <DType T>
@@ -249,18 +269,17 @@ __device__ __forceinline__ float chunk_max(const uint4 &c) {
 
 // The sums of U more chunks, their maxima first; chunk u counts where used[u].
 template <DType T, bool REF, int U>
-__device__ __forceinline__ void add_chunks(RowStats &r, const uint4 *zc, const uint4 *qc, const bool *used, float kz, float kq) {
-    float M = r.M, Mq = r.Mq;
+__device__ __forceinline__ void add_chunks(Sums &s, const uint4 *zc, const uint4 *qc, const bool *used, float kz, float kq) {
+    float M = s.r.M, Mq = s.r.Mq;
 #pragma unroll
     for (int u = 0; u < U; ++u) {  // a thread's maximum is one of its own chunks'
         M = fmaxf(M, used[u] ? chunk_max<T>(zc[u]) : kLowest);
         if (REF) Mq = fmaxf(Mq, used[u] ? chunk_max<T>(qc[u]) : kLowest);
     }
-    rebase<REF>(r, M, Mq, kz, kq);
-    const Scale sz = scale_of(M, kz), sq = scale_of(Mq, kq);
+    rebase<REF>(s, M, Mq, kz, kq);
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (used[u]) add_chunk<T, REF>(r, zc[u], REF ? qc[u] : zc[u], sz, sq);
+        if (used[u]) add_chunk<T, REF>(s.r, zc[u], REF ? qc[u] : zc[u], s.z, s.q);
 }
 
 // What the gradient of a row needs: dz = 2^x (A x - C y + B), plus `at` at the token.
@@ -399,12 +418,13 @@ __device__ __forceinline__ void sum_lanes(RowStats &r) {
 // has the maximum, once), that thread's chunks are read again and added without it; s is then the sum of the
 // others, and top 1.  Thread t's chunks are first + t, first + t + NT, ... below last.
 template <DType T, bool REF, int NT>
-__device__ __forceinline__ RowStats join_threads(RowStats r, const RowArgs &a, const Row<T> &row, int first, int last) {
+__device__ __forceinline__ RowStats join_threads(Sums s, const RowArgs &a, const Row<T> &row, int first, int last) {
     constexpr int NW = NT / 64, N = Chunk<T>::N;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    RowStats &r = s.r;
     const float M = wave_max(r.M), Mq = REF ? wave_max(r.Mq) : kLowest;
     const bool mine = r.M == M;
-    rebase<REF>(r, M, Mq, a.kz, a.kq);
+    rebase<REF>(s, M, Mq, a.kz, a.kq);
     float other = wave_sum(mine ? 0.f : r.s), who = wave_max(mine ? (float)threadIdx.x : -1.f);
     sum_lanes<REF>(r);
     if (NW > 1) {
@@ -422,15 +442,17 @@ __device__ __forceinline__ RowStats join_threads(RowStats r, const RowArgs &a, c
         const float za = r.za;
         r = waves[l];
         r.za = za;
+        s.z = scale_of(r.M, a.kz);
+        s.q = scale_of(r.Mq, a.kq);
         const float Mw = wave_max(r.M), Mqw = REF ? wave_max(r.Mq) : kLowest;
         const bool has = r.M == Mw;
-        rebase<REF>(r, Mw, Mqw, a.kz, a.kq);
+        rebase<REF>(s, Mw, Mqw, a.kz, a.kq);
         other = wave_sum(in ? (has ? others[l] : r.s) : 0.f);
         who = wave_max(in && has ? whos[l] : -1.f);
         if (!in) r.s = r.t = r.k = r.sq = 0.f;
         sum_lanes<REF>(r);
     }
-    const Scale sz = scale_of(r.M, a.kz);
+    const Scale sz = s.z;
     if (r.s < 1.5f * __builtin_amdgcn_exp2f(sz.of(r.M)) && r.s > 0.f) {
         float own = 0.f;
         for (int c = first + (int)who + lane * NT; c < last; c += 64 * NT) {
@@ -514,11 +536,22 @@ __global__ void __launch_bounds__(NT) row_kernel(RowArgs a) {
             if (REF) qr[c] = row.template load<true>(row.q, cc);
         }
     }
-    RowStats r = {kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, St<T>::load(row.z, row.at), 0.f};
+    Sums s = no_sums(St<T>::load(row.z, row.at), a.kz, a.kq);
     if (NC > 0 && T == DType::BF16 && row.lead && tid == 0) {
         row.first(zr[0]);
         if (REF) row.first(qr[0]);
     }
+    constexpr int G = 2;  // chunks between two looks at the maximum
+    static_assert(NC % G == 0, "whole groups");
+#pragma unroll
+    for (int c = 0; c < NC; c += G)
+        if (c * NT < nfull) {
+            bool used[G];
+#pragma unroll
+            for (int u = 0; u < G; ++u) used[u] = tid + (c + u) * NT < nfull;
+            // the second of a group may lie wholly past the row and hold -inf, which adds nothing
+            add_chunks<T, REF, G>(s, zr + c, REF ? qr + c : zr + c, used, a.kz, a.kq);
+        }
     if (BIG) {
         constexpr int U = REF ? 2 : 4;
         static_assert(SL % U == 0, "a round of loads is kept whole or not at all");
@@ -545,7 +578,7 @@ __global__ void __launch_bounds__(NT) row_kernel(RowArgs a) {
                     if (REF) kept[((slot + u) * P + 1) * NT + tid] = qc[u];
                 }
             }
-            add_chunks<T, REF, U>(r, zc, REF ? qc : zc, used, a.kz, a.kq);
+            add_chunks<T, REF, U>(s, zc, REF ? qc : zc, used, a.kz, a.kq);
         };
         int c = NC * NT + tid;
 #pragma unroll 1
@@ -553,25 +586,13 @@ __global__ void __launch_bounds__(NT) row_kernel(RowArgs a) {
 #pragma unroll 1
         for (; c < nfull; c += NT * U) round(c, -1, std::integral_constant<bool, NC == 0>{});
     }
-    // one chunk at a time with a reference (two hold more registers: 32000 entries in bf16 95 -> 105 us), else two
-    constexpr int G = REF ? 1 : 2;
-    static_assert(NC % G == 0, "whole groups");
-#pragma unroll
-    for (int c = 0; c < NC; c += G)
-        if (c * NT < nfull) {
-            bool used[G];
-#pragma unroll
-            for (int u = 0; u < G; ++u) used[u] = tid + (c + u) * NT < nfull;
-            // the second of a group may lie wholly past the row and hold -inf, which adds nothing
-            add_chunks<T, REF, G>(r, zr + c, REF ? qr + c : zr + c, used, a.kz, a.kq);
-        }
     const bool ends = nfull < nch && tid == nfull % NT;  // the row's last elements are this thread's
     if (ends) {
         const uint4 zt = Chunk<T>::tail(row.z, row.V), qt = REF ? Chunk<T>::tail(row.q, row.V) : none;
         const bool used = true;
-        add_chunks<T, REF, 1>(r, &zt, &qt, &used, a.kz, a.kq);
+        add_chunks<T, REF, 1>(s, &zt, &qt, &used, a.kz, a.kq);
     }
-    r = join_threads<T, REF, NT>(r, a, row, 0, nch);
+    const RowStats r = join_threads<T, REF, NT>(s, a, row, 0, nch);
     if (tid < 64) {
         const RowCoef c = finish_row(a, i, in, r, true);
         if (tid == 0) coef = c;
@@ -579,6 +600,15 @@ __global__ void __launch_bounds__(NT) row_kernel(RowArgs a) {
     if (NC == 0) return;
     __syncthreads();
     const RowCoef rc = uniform(coef);
+    if (BIG) {  // what has to be read again first: it was read last, and the L2 may still hold it
+        for (int c = (NC + SL) * NT + tid; c < nfull; c += NT) {
+            const uint4 zc = row.template load<false>(row.z, c), qc = REF ? row.template load<false>(row.q, c) : zc;
+            st16_once((uint8_t *)row.dz + (uint32_t)c * 16u, grad_of<T, REF>(rc, c, row.at, zc, qc));
+        }
+        for (int slot = 0, c = NC * NT + tid; slot < SL && c < nfull; ++slot, c += NT)
+            st16_once((uint8_t *)row.dz + (uint32_t)c * 16u,
+                      grad_of<T, REF>(rc, c, row.at, kept[slot * P * NT + tid], kept[(slot * P + P - 1) * NT + tid]));
+    }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int cc = tid + c * NT;
@@ -588,16 +618,6 @@ __global__ void __launch_bounds__(NT) row_kernel(RowArgs a) {
                 row.store(cc, g);
             else
                 st16_once((uint8_t *)row.dz + (uint32_t)cc * 16u, g);
-        }
-    }
-    if (BIG) {
-        int c = NC * NT + tid;
-        for (int slot = 0; slot < SL && c < nfull; ++slot, c += NT)
-            st16_once((uint8_t *)row.dz + (uint32_t)c * 16u,
-                      grad_of<T, REF>(rc, c, row.at, kept[slot * P * NT + tid], kept[(slot * P + P - 1) * NT + tid]));
-        for (; c < nfull; c += NT) {
-            const uint4 zc = row.template load<false>(row.z, c), qc = REF ? row.template load<false>(row.q, c) : zc;
-            st16_once((uint8_t *)row.dz + (uint32_t)c * 16u, grad_of<T, REF>(rc, c, row.at, zc, qc));
         }
     }
     if (ends) {
@@ -622,7 +642,7 @@ __global__ void __launch_bounds__(kPartThreads) row_part_kernel(RowArgs a, int S
     const Row<T> row(a, i, in.tok, REF);
     const int first = p * per, last = min(row.nch, first + per), whole = min(row.nfull, last);
     const int own = row.at / N;
-    RowStats r = {kLowest, 0.f, 0.f, 0.f, kLowest, 0.f, own >= first && own < last ? St<T>::load(row.z, row.at) : 0.f, 0.f};
+    Sums s = no_sums(own >= first && own < last ? St<T>::load(row.z, row.at) : 0.f, a.kz, a.kq);
     for (int c = first + tid; c < whole; c += NT * U) {
         uint4 zc[U], qc[U];
         bool used[U];
@@ -637,14 +657,14 @@ __global__ void __launch_bounds__(kPartThreads) row_part_kernel(RowArgs a, int S
             row.first(zc[0]);
             if (REF) row.first(qc[0]);
         }
-        add_chunks<T, REF, U>(r, zc, REF ? qc : zc, used, a.kz, a.kq);
+        add_chunks<T, REF, U>(s, zc, REF ? qc : zc, used, a.kz, a.kq);
     }
     if (last > row.nfull && first <= row.nfull && tid == (row.nfull - first) % NT) {  // the row's end is in this part
         const uint4 zt = Chunk<T>::tail(row.z, row.V), qt = REF ? Chunk<T>::tail(row.q, row.V) : zt;
         const bool used = true;
-        add_chunks<T, REF, 1>(r, &zt, &qt, &used, a.kz, a.kq);
+        add_chunks<T, REF, 1>(s, &zt, &qt, &used, a.kz, a.kq);
     }
-    r = join_threads<T, REF, NT>(r, a, row, first, last);
+    const RowStats r = join_threads<T, REF, NT>(s, a, row, first, last);
     if (tid == 0) a.part[i * S + p] = r;
 }
 
@@ -654,13 +674,17 @@ template <bool REF>
 __device__ __forceinline__ RowStats join_parts(const RowArgs &a, long i, int S, int own) {
     const int lane = threadIdx.x & 63;
     const bool in = lane < S;
-    RowStats r = a.part[i * S + min(lane, S - 1)];
+    Sums s;
+    RowStats &r = s.r;
+    r = a.part[i * S + min(lane, S - 1)];
+    s.z = scale_of(r.M, a.kz);
+    s.q = scale_of(r.Mq, a.kq);
     const float M = wave_max(r.M), Mq = REF ? wave_max(r.Mq) : kLowest;
     if (r.M != M) {
-        r.s += r.top * __builtin_amdgcn_exp2f(scale_of(r.M, a.kz).of(r.M));
+        r.s += r.top * __builtin_amdgcn_exp2f(s.z.of(r.M));
         r.top = 0.f;
     }
-    rebase<REF>(r, M, Mq, a.kz, a.kq);
+    rebase<REF>(s, M, Mq, a.kz, a.kq);
     if (!in) r.s = r.t = r.k = r.sq = r.top = 0.f;
     sum_lanes<REF>(r);
     r.top = wave_sum(r.top);
