@@ -309,7 +309,7 @@ const char *dvi_op_error(void);
 
 /*
  * Rows of logits: DEVICE [rows, vocab] of dtype, row i at logits + i * ld elements (ld >= 0, any
- * alignment of its elements; rows may overlap, as an expanded row's do; at most 2^22 rows of at most 2^28
+ * alignment of its elements; rows may overlap, as an expanded row's do; at most 2^21 rows of at most 2^28
  * entries); temperature, from 1e-6 to 1e6, divides them.
  * tokens: DEVICE int32 [rows].  A row whose token lies outside [0, vocab) or that has no logit above
  * -inf is masked: its outputs are 0.  Logits of -inf (or the type's lowest number) are tokens of

@@ -1522,7 +1522,7 @@ static bool rows_apart(const void *p, int64_t pld, const void *q, int64_t qld, i
 // The largest number of rows (a launch's threads are counted in 32 bits), the widest stride, and the largest
 // vocabulary (a row's bytes are counted in 32 bits).
 static constexpr int32_t kMaxOpVocab = 1 << 28;
-static constexpr int64_t kMaxOpRows = (int64_t)1 << 22, kMaxOpStride = (int64_t)1 << 36;
+static constexpr int64_t kMaxOpRows = (int64_t)1 << 21, kMaxOpStride = (int64_t)1 << 36;
 
 static dvi_status check_rows(int64_t rows, int32_t vocab, dvi_dtype dtype, const void *logits, int64_t ld,
                              const int32_t *tokens, double temperature) {

@@ -403,7 +403,7 @@ def test_large_offsets():
     check_policy(learn().policy_loss(z, tok, **d, **kw, out=z), want, BF16, V)
 
 
-@pytest.mark.parametrize("n,V", [(2, 70000), (300, 700)])
+@pytest.mark.parametrize("n,V", [(2, 70000), (300, 700), (130, 70001)])
 def test_captured_and_on_other_streams(n, V):
     z, tok, d = make_policy(n, V, F32, "logits")
     kw = dict(clip_low=LO, clip_high=HI, c_kl=0.3, c_ent=0.02)
