@@ -307,7 +307,7 @@ static size_t layout(dvi_ctx *x, const dvi_config &c, void *base) {
     float *ring_old = b.take<float>(R * 4);
     float *pol_logp = b.take<float>(R * 4);
     float *pol_terms = b.take<float>(8 * 4);
-    void *op_ws = b.take<void>(std::max(rows_workspace((long)R, (int)V, true), (size_t)kNormGrid * sizeof(double)));
+    void *op_ws = b.take<void>(std::max(rows_workspace_up_to((long)R, (int)V, true), (size_t)kNormGrid * sizeof(double)));
     if (x && base) {
         x->L = Ls;
         x->emb = emb; x->head = head; x->final_norm = final_norm; x->rope = rope;

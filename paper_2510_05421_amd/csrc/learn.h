@@ -46,6 +46,8 @@ struct RowArgs {
 
 // Workspace of launch_rows in bytes (any dtype, with or without reference).
 size_t rows_workspace(long N, int V, bool policy);
+// The same for N rows or any smaller number of them (fewer rows may take more: they are split).
+size_t rows_workspace_up_to(long N, int V, bool policy);
 void launch_rows(DType t, RowArgs a, void *workspace, hipStream_t s);
 
 // ---- AdamW ----

@@ -784,6 +784,13 @@ size_t rows_workspace(long N, int V, bool policy) {
     return (S > 1 ? up256((size_t)N * 64 * sizeof(RowStats)) : 0) + (policy ? up256((size_t)N * 32) : 0);
 }
 
+size_t rows_workspace_up_to(long N, int V, bool policy) {
+    int per;
+    const bool split = N > 0 && row_parts(1, (V + 3) / 4, policy, per) > 1;  // as one row is, if any number is
+    const long few = std::min<long>(N, compute_units() / 4);                 // more are not
+    return (split ? up256((size_t)few * 64 * sizeof(RowStats)) : 0) + (policy ? up256((size_t)N * 32) : 0);
+}
+
 template <DType T, bool REF, int NT, int NC, int SL = 0, bool BIG = false>
 static void launch_row_shape(const RowArgs &a, hipStream_t s) {
     constexpr int lds = SL * (REF ? 2 : 1) * NT * 16;

@@ -106,6 +106,22 @@ def test_updates_reuse_the_rows(rows, vocab, rank, bf16):
     eng.close()
 
 
+def test_a_ring_that_is_partly_full_stays_in_its_workspace():
+    """Few rows of a large vocabulary are split over workgroups, whose sums take more room than the rows of a full
+    ring do: nothing behind the workspace is written."""
+    shape = TINY.replace(vocab=33024)
+    eng, buf, W = setup(shape, 30, buffer_rows=200)
+    nbytes = eng.lib.dvi_workspace_bytes(ctypes.byref(eng._ccfg))
+    behind = eng.workspace[-eng.workspace.data_ptr() % 256 + nbytes:]
+    assert 0 < behind.numel() <= 256
+    behind.fill_(0xa5)
+    A, B = factors(eng)
+    st = eng.update_policy(**COEF, lr=0.0, grads=True)
+    check(st, ref(W, A, B, shape, buf, np.full(30, np.nan)))
+    assert (behind == 0xa5).all()
+    eng.close()
+
+
 def test_rows_that_another_update_used_keep_their_log_probabilities():
     """The drafter update clears the fresh flags and keeps what the policy update needs."""
     shape = TINY
