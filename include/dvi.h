@@ -382,7 +382,7 @@ dvi_status dvi_policy_loss(const dvi_policy_args *args, void *workspace, size_t 
  * max_norm > 0: the norm of all gradients together goes to grad_norm (NULL or DEVICE fp32 [1]); a norm
  * above max_norm scales the gradients down to it, and one that is not finite leaves every tensor and
  * state as it is.  max_norm = +inf only measures and guards; with 0 nothing is measured, and
- * grad_norm must be NULL.
+ * grad_norm must be NULL.  eps is at least 2^-126 (below, fp32 may hold it as 0).
  * Parameters of dtype, gradients of grad_dtype.  master: NULL, or the fp32 values that a bf16 parameter
  * is the rounding of (then all tensors have one).
  * state_bits 32: m and v are fp32.  state_bits 8: m and v hold OCP e4m3 codes of m and of sqrt(v), times

@@ -4,6 +4,7 @@
 // update (Section 3.4) is dvi_update_drafter.  All device work is enqueued on the context's
 // stream; host bookkeeping (lengths, ring occupancy) mirrors the device so capacity and state
 // errors are caught before anything is launched.
+#include <float.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -1255,7 +1256,7 @@ static const char *check_adam(const dvi_ctx *x, float lr, float beta1, float bet
     if (!x->adamw || lr == 0.f) return nullptr;
     if (!isfinite(lr)) return "lr must be finite";
     if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f)) return "0 <= beta1, beta2 < 1";
-    if (!(eps > 0.f) || !isfinite(eps)) return "eps must be > 0";
+    if (!(eps >= FLT_MIN) || !isfinite(eps)) return "eps must be from 2^-126 to the largest fp32";
     return nullptr;
 }
 
@@ -1656,7 +1657,7 @@ static AdamArgs adam_numbers(double lr, double beta1, double beta2, double eps, 
     a.rate = (float)(lr / (1.0 - pow(beta1, step)));
     a.root = (float)(1.0 / sqrt(1.0 - pow(beta2, step)));
     a.eps = (float)eps;
-    a.max_norm = (float)max_norm;
+    a.max_norm = max_norm;
     step_keys(seed, step, a.key0, a.key1);
     return a;
 }
@@ -1679,7 +1680,7 @@ static void launch_adam_step(DType pt, bool master, DType gt, int bits, const dv
                              AdamArgs a, double *part, float *norm, hipStream_t s) {
     AdamTensor t[kAdamTensors];
     long base = 0;
-    if (a.max_norm > 0.f) {
+    if (a.max_norm > 0.0) {
         a.norm_part = part;
         for (int at = 0, n; (n = adam_group(tensors, n_tensors, at, base, t)) > 0;) {
             launch_adam_norm(gt, t, n, part + a.n_part, s);
@@ -1703,7 +1704,10 @@ extern "C" dvi_status dvi_adamw(const dvi_adamw_tensor *tensors, int32_t n_tenso
     if (!isfinite(g->lr) || !isfinite(g->weight_decay)) return op_fail(DVI_ERR_ARG, "lr and weight_decay must be finite");
     if (!(g->beta1 >= 0.0 && g->beta1 < 1.0) || !(g->beta2 >= 0.0 && g->beta2 < 1.0))
         return op_fail(DVI_ERR_ARG, "0 <= beta1, beta2 < 1");
-    if (!(g->eps > 0.0) || !isfinite(g->eps)) return op_fail(DVI_ERR_ARG, "eps must be > 0");
+    // in fp32, as the step uses them
+    if (!(g->eps >= FLT_MIN && g->eps <= FLT_MAX)) return op_fail(DVI_ERR_ARG, "eps must be from 2^-126 to the largest fp32");
+    if (fabs(g->lr) > FLT_MAX || fabs(g->lr * g->weight_decay) > FLT_MAX)
+        return op_fail(DVI_ERR_ARG, "lr and lr weight_decay must be in fp32's range");
     if (!(g->max_norm >= 0.0)) return op_fail(DVI_ERR_ARG, "max_norm must not be negative");
     if (g->grad_norm && g->max_norm == 0.0) return op_fail(DVI_ERR_ARG, "grad_norm needs max_norm > 0");
     int masters = 0, used = 0;

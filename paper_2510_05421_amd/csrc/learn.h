@@ -67,7 +67,8 @@ struct AdamTensor {
     long base;        // 8 bits: number of the first element's random bits
 };
 struct AdamArgs {
-    float b1, one_b1, b2, one_b2, decay, rate, root, eps, max_norm;
+    float b1, one_b1, b2, one_b2, decay, rate, root, eps;
+    double max_norm;
     uint32_t key0, key1;
     const double *norm_part;  // partial sums of squares, n_part of them, or nullptr
     int n_part;

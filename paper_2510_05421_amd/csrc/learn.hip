@@ -1092,7 +1092,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamTable tab, AdamArgs a) {
         const double norm = norm_of(a.norm_part, a.n_part, red);
         if (a.norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) a.norm[0] = (float)norm;
         if (!(norm <= 1.7e308)) return;  // a gradient that is not finite: no step
-        if (norm > (double)a.max_norm) clip = (float)((double)a.max_norm / norm);
+        if (norm > a.max_norm) clip = (float)(a.max_norm / norm);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {

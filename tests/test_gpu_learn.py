@@ -557,6 +557,17 @@ def test_adamw_many_tensors(count):
         assert ((params[i].cpu().double() - p[i]).abs() <= 24 * U * 0.02 + 4 * U * p[i].abs()).all()
 
 
+def test_adamw_clips_to_a_norm_that_fp32_holds_as_zero():
+    params, grads = adam_inputs([700, 300], F32, F32)
+    before = [p.clone() for p in params]
+    opt = learn().AdamW(params, lr=1e-2, max_norm=1e-60)
+    opt.step(grads[0])
+    norm = sum((g.cpu().double() ** 2).sum().item() for g in grads[0]) ** 0.5
+    assert abs(opt.grad_norm.item() - norm) <= 2 * U * norm
+    # the gradients times 1e-60 / norm are below fp32: m and v stay 0, and so does the step
+    assert all(torch.equal(a, b) for a, b in zip(before, params))
+
+
 def codes(states, i, n, name):
     s = states[name + "_scale"][i].cpu().double().repeat_interleave(256)[:n]
     return states[name][i].cpu().to(torch.float32).double() * s

@@ -69,7 +69,8 @@ def test_policy_loss_refuses(kw):
 
 @pytest.mark.parametrize("tensor,kw", [
     ({}, dict(dtype=3)), ({}, dict(grad_dtype=3)), ({}, dict(state_bits=16)), ({}, dict(step=0)), ({}, dict(lr=NAN)),
-    ({}, dict(beta1=1.0)), ({}, dict(beta2=-0.1)), ({}, dict(beta2=NAN)), ({}, dict(eps=0.0)), ({}, dict(max_norm=-1.0)),
+    ({}, dict(beta1=1.0)), ({}, dict(beta2=-0.1)), ({}, dict(beta2=NAN)), ({}, dict(eps=0.0)), ({}, dict(eps=1e-50)), ({}, dict(lr=1e200)),
+    ({}, dict(lr=1e30, weight_decay=1e30)), ({}, dict(max_norm=-1.0)),
     ({}, dict(max_norm=NAN)), ({}, dict(weight_decay=INF)), ({}, dict(grad_norm=A)), ({}, dict(state_bits=8)),
     (dict(n=-1), {}), (dict(param=None), {}), (dict(grad=None), {}), (dict(m=None), {}), (dict(v=None), {}),
     (dict(master=D), {}), (dict(master=D), dict(dtype=_abi.BF16)), (dict(param=A + 2), {}), (dict(m=C + 2), {}),
