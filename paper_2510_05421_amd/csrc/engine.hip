@@ -1687,6 +1687,10 @@ static void launch_adam_step(DType pt, bool master, DType gt, int bits, const dv
             a.n_part += adam_norm_parts(t, n);
         }
         if (a.n_part == 0 && norm) launch_adam_norm_out(part, 0, norm, s);
+        if (a.n_part > kNormDirect) {
+            launch_adam_norm_join(part, a.n_part, s);
+            a.n_part = 1;
+        }
     }
     a.norm = norm;
     base = 0;

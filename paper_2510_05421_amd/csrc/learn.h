@@ -56,6 +56,7 @@ constexpr int kAdamTensors = 48;   // tensors of one launch: their table is a ke
 constexpr int kAdamChunk = 1024;   // elements of a tensor that a workgroup takes at least
 constexpr int kNormChunk = 8192;   // elements that a workgroup of the norm takes at a time
 constexpr int kNormGrid = 2048;    // workgroups, and so partial sums, of a launch of the norm
+constexpr int kNormDirect = 256;   // up to so many partial sums every workgroup of the step adds itself
 
 struct AdamTensor {
     long n;
@@ -79,6 +80,8 @@ int adam_norm_parts(const AdamTensor *t, int n);
 void launch_adam_norm(DType gt, const AdamTensor *t, int n, double *part, hipStream_t s);
 // One launch for up to kAdamTensors tensors.
 void launch_adamw(DType pt, bool master, DType gt, int bits, const AdamTensor *t, int n, const AdamArgs &a, hipStream_t s);
+// One partial sum, part[0], for n_part of them.
+void launch_adam_norm_join(double *part, int n_part, hipStream_t s);
 // The norm alone, for a call without any element.
 void launch_adam_norm_out(const double *part, int n_part, float *norm, hipStream_t s);
 

@@ -1006,20 +1006,28 @@ __global__ void __launch_bounds__(256) adam_norm_kernel(NormTable tab, double *p
     if (threadIdx.x == 0) part[blockIdx.x] = ((red[0] + red[1]) + red[2]) + red[3];
 }
 
-// The norm out of the partial sums, the same in every workgroup.
-__device__ __forceinline__ double norm_of(const double *part, int n, double *red4) {
+// The sum of the partial sums, the same in every workgroup.
+__device__ __forceinline__ double sum_parts(const double *part, int n, double *red4) {
     double s = 0.0;
     for (int i = threadIdx.x; i < n; i += 256) s += part[i];
     s = wave_sum_f64(s);
     if ((threadIdx.x & 63) == 0) red4[threadIdx.x >> 6] = s;
     __syncthreads();
-    return sqrt(((red4[0] + red4[1]) + red4[2]) + red4[3]);
+    return ((red4[0] + red4[1]) + red4[2]) + red4[3];
+}
+
+// Many partial sums become one, in the place of the first (which every thread has read by then), before the
+// step's workgroups all read them.
+__global__ void __launch_bounds__(256) adam_norm_join_kernel(double *part, int n) {
+    __shared__ double red[4];
+    const double s = sum_parts(part, n, red);
+    if (threadIdx.x == 0) part[0] = s;
 }
 
 __global__ void __launch_bounds__(256) adam_norm_out_kernel(const double *part, int n, float *norm) {
     __shared__ double red[4];
-    const double v = norm_of(part, n, red);
-    if (threadIdx.x == 0) norm[0] = (float)v;
+    const double v = sum_parts(part, n, red);
+    if (threadIdx.x == 0) norm[0] = (float)sqrt(v);
 }
 
 // 32 random bits for element number `at` of the step with these keys: xorshifts and multiplications whose
@@ -1089,7 +1097,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamTable tab, AdamArgs a) {
     }
     float clip = 1.f;
     if (a.norm_part != nullptr) {  // while the loads are on their way
-        const double norm = norm_of(a.norm_part, a.n_part, red);
+        const double norm = sqrt(sum_parts(a.norm_part, a.n_part, red));
         if (a.norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) a.norm[0] = (float)norm;
         if (!(norm <= 1.7e308)) return;  // a gradient that is not finite: no step
         if (norm > a.max_norm) clip = (float)(a.max_norm / norm);
@@ -1184,6 +1192,10 @@ void launch_adam_norm(DType gt, const AdamTensor *t, int n, double *part, hipStr
         adam_norm_kernel<DType::BF16><<<grid, 256, 0, s>>>(tab, part);
     else
         adam_norm_kernel<DType::F32><<<grid, 256, 0, s>>>(tab, part);
+}
+
+void launch_adam_norm_join(double *part, int n_part, hipStream_t s) {
+    adam_norm_join_kernel<<<1, 256, 0, s>>>(part, n_part);
 }
 
 void launch_adam_norm_out(const double *part, int n_part, float *norm, hipStream_t s) {

@@ -568,6 +568,22 @@ def test_adamw_clips_to_a_norm_that_fp32_holds_as_zero():
     assert all(torch.equal(a, b) for a, b in zip(before, params))
 
 
+def test_adamw_norm_of_more_parts_than_one_launch_makes():
+    """60 tensors of 300000 elements: 2220 partial sums of two launches, made one before the step."""
+    params, grads = adam_inputs([300000] * 60, F32, F32)
+    opt = learn().AdamW(params, lr=1e-2, max_norm=0.5)
+    once = [p.clone() for p in params]
+    opt.step(grads[0])
+    norm = sum((g.double() ** 2).sum().item() for g in grads[0]) ** 0.5
+    assert abs(opt.grad_norm.item() - norm) <= 2 * U * norm
+    # the same step from gradients that are clipped already, to a rounding of the scale and one of the product
+    two = learn().AdamW(once, lr=1e-2)
+    two.step([g * (0.5 / norm) for g in grads[0]])
+    for i in (0, 47, 48, 59):
+        # m / sqrt(v) is one at the first step: 24 roundings of it, as above
+        assert ((params[i] - once[i]).abs() <= 24 * U * 0.02 + 4 * U * once[i].abs()).all()
+
+
 def codes(states, i, n, name):
     s = states[name + "_scale"][i].cpu().double().repeat_interleave(256)[:n]
     return states[name][i].cpu().to(torch.float32).double() * s
