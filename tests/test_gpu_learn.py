@@ -403,6 +403,27 @@ def test_large_offsets():
     check_policy(learn().policy_loss(z, tok, **d, **kw, out=z), want, BF16, V)
 
 
+def test_a_million_rows():
+    """More rows than any grid of a smaller dimension takes: each of them one of 64 of the oracle's."""
+    n, V = 1 << 20, 9
+    z0, tok0, d0 = make_policy(64, V, F32, "tokens", seed=4)
+    z, tok, d = z0.repeat(n // 64, 1), tok0.repeat(n // 64), {k: v.repeat(n // 64) for k, v in d0.items()}
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.3, c_ent=0.02)
+    want = oracle(z0, tok0, **d0, **kw)
+    got = learn().policy_loss(z, tok, **d, **kw)
+    part = learn().policy_loss(z0, tok0, **d0, **kw)
+    check_policy(part, want, F32, V)
+    assert torch.equal(got.grad.view(n // 64, 64, V), part.grad.expand(n // 64, 64, V))
+    assert torch.equal(got.logp.view(n // 64, 64), part.logp.expand(n // 64, 64))
+    # the terms are sums of 64-bit numbers, rounded once
+    sums = want["terms"] * (n // 64)
+    assert ((got.terms.cpu().double() - sums).abs() <= 2 * tol(want["R"], V) * want["tmag"] * (n // 64)).all()
+    logp, ent = learn().token_logprobs(z, tok, entropy=True)
+    few, fent = learn().token_logprobs(z0, tok0, entropy=True)
+    assert torch.equal(logp.view(n // 64, 64), few.expand(n // 64, 64))
+    assert torch.equal(ent.view(n // 64, 64), fent.expand(n // 64, 64))
+
+
 @pytest.mark.parametrize("n,V", [(2, 70000), (300, 700), (130, 70001)])
 def test_captured_and_on_other_streams(n, V):
     z, tok, d = make_policy(n, V, F32, "logits")
@@ -634,6 +655,46 @@ def test_adamw_8bit(dtype, gdtype, master, max_norm, skip):
                 assert ((held - x).abs() <= spacing(x, sc) * (1 + 1e-4)).all(), (k, s, name)
                 if name == "r":
                     assert (held[x > 0] > 0).all()
+
+
+@pytest.mark.parametrize("dtype,gdtype,master", [(F32, F32, False), (F32, BF16, False), (BF16, BF16, True), (BF16, F32, True),
+                                                 (BF16, BF16, False), (BF16, F32, False)])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_large_steps_are_the_small_ones(bits, dtype, gdtype, master):
+    """A step that goes past the caches (30 million elements move more than 256 MiB in every form) gives the
+    bits of steps over pieces of it: all pieces with 32-bit states; with 8 bits, whose random bits count
+    from the first tensor, the first piece, and the last block by the formula (spacings of e4m3 apart at most)."""
+    n, piece = 30_000_003, 4_999_936      # a multiple of 256
+    g = torch.Generator(device="cuda").manual_seed(5)
+    p = torch.randn(n + 1, generator=g, device="cuda").to(dtype)[1:]
+    grads = [(torch.randn(n + 1, generator=g, device="cuda") * 0.01).to(gdtype)[1:] for _ in range(2)]
+    kw = dict(lr=1e-2, weight_decay=0.1, max_norm=math.inf, state_bits=bits, seed=3, master=master)
+    spans = [slice(i, i + piece) for i in range(0, n, piece)][:1 if bits == 8 else None]
+    small = [p[c].clone() for c in spans]
+    one = learn().AdamW([p], **kw)
+    many = [learn().AdamW([x], **kw) for x in small]
+    for gr in grads:
+        one.step([gr])
+        for o, c in zip(many, spans):
+            o.step([gr[c]])
+    norm = grads[1].double().square().sum().sqrt().item()
+    assert abs(one.grad_norm.item() - norm) <= 2 * U * norm
+    for o, x, c in zip(many, small, spans):
+        assert torch.equal(p[c], x)
+        for k, t in o.states.items():
+            at = slice(c.start // 256, c.start // 256 + t[0].numel()) if k.endswith("scale") else c
+            assert torch.equal(one.states[k][0][at].view(torch.uint8), t[0].view(torch.uint8)), k
+    if bits == 8:
+        first = learn().AdamW([p.clone()], **kw)
+        first.step([grads[0]])
+        tail = n % 256                    # the last block
+        gt = grads[0][-tail:].cpu().double()
+        for name, want in (("m", 0.1 * gt), ("r", (0.001 ** 0.5) * gt.abs())):
+            sc = first.states[name + "_scale"][0][-1].cpu().double()
+            # 1 - beta in fp32 is 2^-25 off beta, 3e-7 and 3e-5 of itself at most
+            assert abs(sc - want.abs().max() / 448) <= 5e-5 * sc
+            held = first.states[name][0][-tail:].cpu().float().double() * sc
+            assert ((held - want).abs() <= spacing(want, sc) * (1 + 1e-3)).all()
 
 
 def test_adamw_8bit_rounds_with_the_exact_mean():
