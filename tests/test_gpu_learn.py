@@ -403,6 +403,40 @@ def test_large_offsets():
     check_policy(learn().policy_loss(z, tok, **d, **kw, out=z), want, BF16, V)
 
 
+@pytest.mark.parametrize("dtype,n,V", [(F32, 1, 1 << 28), (BF16, 1, (1 << 28) - 3), (BF16, 70, (1 << 22) + 5)])
+def test_the_longest_rows(dtype, n, V):
+    """Rows up to 2^28 entries, in parts (one row) and whole (70 rows), against 64 bits on the device.  A thread
+    adds at most V / 1024 of its entries in a row, and the maximum's rescaling costs no more than the chain."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.randn(n, V, generator=g, device="cuda").to(dtype)
+    tok = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    tok[0] = V - 1
+    adv = torch.full((n,), 0.7, device="cuda")
+    out = learn().policy_loss(z, tok, adv, c_ent=0.5)
+    logp, ent = learn().token_logprobs(z, tok, entropy=True)
+    t = (8 * 16 + V / 1024 + 64) * U
+    loss = 0.0
+    for i in range(n):
+        lg = torch.log_softmax(z[i].double(), -1)
+        p = lg.exp()
+        H, lp = -(p * lg).sum().item(), lg[tok[i].long()].item()
+        assert abs(logp[i].item() - lp) <= t + U * abs(lp) and out.logp[i].item() == pytest.approx(lp, abs=t + U * abs(lp))
+        assert abs(ent[i].item() - H) <= t * (1 + 2 * H)
+        loss += (-0.7 - 0.5 * H) / n
+        if i in (0, n - 1):
+            grad = p * (0.5 * (lg + H) + 0.7) / n
+            mag = p * (0.5 * (lg.abs() + H) + 0.7) / n
+            grad[tok[i].long()] -= 0.7 / n
+            off = (out.grad[i].double() - grad).abs() - (2 * t * mag + half_step(dtype) * grad.abs() * 1.01 + 1e-37)
+            at = off.argmax().item()
+            if at == tok[i].item():       # the token's own term, beside its share of the others
+                off[at] -= 0.7 / n * 4 * U
+            assert off.max().item() <= 0, (i, at, off.max().item())
+            del grad, mag, off
+        del lg, p
+    assert abs(out.terms[0].item() - loss) <= 2 * t * (0.7 + 0.5 * 2 * 20)
+
+
 def test_a_million_rows():
     """More rows than any grid of a smaller dimension takes: each of them one of 64 of the oracle's."""
     n, V = 1 << 20, 9
