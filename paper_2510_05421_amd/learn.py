@@ -3,7 +3,8 @@ gradient, and AdamW over many tensors with states in 32 or 8 bits.
 
 Each call runs in the HIP kernels behind the C entry point of its name (include/dvi.h says what it
 computes), on the current stream of its tensors' device; nothing waits for the device.  Gradients are
-returned by the loss itself: nothing here is recorded by autograd.
+returned by the loss itself: nothing here is recorded by autograd, which does not notice either that a
+step, or a gradient written over its logits, has changed a tensor that some graph still needs.
 """
 from __future__ import annotations
 
