@@ -762,16 +762,22 @@ __global__ void __launch_bounds__(NT) row_terms_kernel(RowArgs a) {
 
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Parts of a row of nch chunks: 1 where its workgroup does the whole row.  A workgroup takes longer for a
-// longer row, and few rows leave most of the chip idle; splitting costs another launch (2.5 us on the host).
-// Whole and split, in us: policy loss with reference logits, fp32: 8 rows of 16000 17.3 and 14.7, of 32000 20.2
-// and 14.3, 48 of 32000 20.7 and 18.0, 1 of 131072 45 and 15, bf16: 8 rows of 32000 15.4 and 14.4, 64 of 131072
-// without reference 28 and 21.5, 128 of 131072 30.7 and 30.7; fp32 with reference 128 of 131072 64 and 71.
-// Log-probabilities, fp32: 4 rows of 32000 8.1 and 8.8, of 131072 15 and 8.8, 64 of 131072 15.3 and 13.4.
-static int row_parts(long N, int nch, bool grad, int &per) {
+// Parts of a row: 1 where its workgroup does the whole row.  A workgroup takes longer for a longer row, and few
+// rows leave most of the chip idle; splitting costs another launch, 2.5 to 3 us of the host's time (3.7 where
+// it also needs the workspace that whole rows do not).  So a row is split where the chip gains more than
+// the host loses: by its entries, which count twice with a reference (a unit is busy with their
+// arithmetic: both types take as long), and by the rows, up to an eighth or a quarter of the units.
+// Whole and split, in us, on the chip alone (and a call by itself where the host is the longer):
+//   with reference, 8 rows of 16000 10.2 and 9.0 (17.2, 19.3), of 32000 13.3 and 9.1 (17.6, 19.8), of 65536 20.8 and
+//   9.6; 48 of 32000 13.8 and 12.2 (17.6, 20.6); 64 of 65536 23.0 and 18.9;
+//   without, 8 rows of 32000 10.4 and 8.1 (16.2, 18.5), of 65536 13.8 and 8.6 (16.4, 18.7), of 131072 21.9 and 9.0;
+//   64 of 65536 14.2 and 12.2 (16.5, 19.1), of 131072 22.0 and 14.8;
+//   log-probabilities, 8 rows of 65536 7.0 and 5.5 (7.7, 11.6), of 131072 10.7 and 5.6 (10.9, 11.7).
+static int row_parts(long N, int V, int nch, bool grad, bool ref, int &per) {
     const int cu = compute_units();
     per = nch;
-    if (N <= 0 || 4 * N > cu || nch < (grad && 8 * N <= cu ? 6000 : 16384)) return 1;
+    const long work = (long)V * (ref ? 2 : 1);
+    if (N <= 0 || 4 * N > cu || work < (grad && 8 * N <= cu ? 49152 : 98304)) return 1;
     const long want = std::min<long>(64, std::min<long>(2L * cu / N, (nch + kPartThreads - 1) / kPartThreads));
     per = (int)((nch + want - 1) / want);
     per = (per + kPartThreads - 1) / kPartThreads * kPartThreads;
@@ -780,13 +786,13 @@ static int row_parts(long N, int nch, bool grad, int &per) {
 
 size_t rows_workspace(long N, int V, bool policy) {
     int per;
-    const int S = row_parts(N, (V + 3) / 4, policy, per);  // as many chunks as any type has
+    const int S = row_parts(N, V, (V + 3) / 4, policy, policy, per);  // as many chunks as any type has
     return (S > 1 ? up256((size_t)N * 64 * sizeof(RowStats)) : 0) + (policy ? up256((size_t)N * 32) : 0);
 }
 
 size_t rows_workspace_up_to(long N, int V, bool policy) {
     int per;
-    const bool split = N > 0 && row_parts(1, (V + 3) / 4, policy, per) > 1;  // as one row is, if any number is
+    const bool split = N > 0 && row_parts(1, V, (V + 3) / 4, policy, policy, per) > 1;  // as one row is, if any number is
     const long few = std::min<long>(N, compute_units() / 4);                 // more are not
     return (split ? up256((size_t)few * 64 * sizeof(RowStats)) : 0) + (policy ? up256((size_t)N * 32) : 0);
 }
@@ -843,7 +849,7 @@ template <DType T, bool REF>
 static void launch_rows_t(RowArgs a, void *workspace, hipStream_t s) {
     const int nch = (a.V + (T == DType::BF16 ? 1 : 0) + Chunk<T>::N - 1) / Chunk<T>::N;  // with a lead
     int per;
-    const int S = row_parts(a.N, nch, a.dz != nullptr, per);
+    const int S = row_parts(a.N, a.V, nch, a.dz != nullptr, REF, per);
     a.row_terms = (double *)workspace;
     a.part = (RowStats *)((uint8_t *)workspace + (a.policy ? up256((size_t)a.N * 32) : 0));
     if (a.N > 0 && S == 1) {
