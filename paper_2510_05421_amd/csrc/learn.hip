@@ -686,9 +686,12 @@ __device__ __forceinline__ RowStats join_parts(const RowArgs &a, long i, int S, 
     s.z = scale_of(r.M, a.kz);
     s.q = scale_of(r.Mq, a.kq);
     const float M = wave_max(r.M), Mq = REF ? wave_max(r.Mq) : kLowest;
+    const float top = r.top * __builtin_amdgcn_exp2f(s.z.of(r.M));
     if (r.M != M) {
-        r.s += r.top * __builtin_amdgcn_exp2f(s.z.of(r.M));
+        r.s += top;
         r.top = 0.f;
+    } else if (REF) {  // its maximum stays, but the reference's may lie in another part
+        r.k -= mul0(top, s.q.b - scale_of(Mq, a.kq).b);
     }
     rebase<REF>(s, M, Mq, a.kz, a.kq);
     if (!in) r.s = r.t = r.k = r.sq = r.top = 0.f;

@@ -327,6 +327,26 @@ def test_likely_tokens_keep_their_digits(n, V, dtype):
     assert ((ent.double() - H).abs() <= 2 * (t + U) * H + 2.0 ** -41 + 2.0 ** -52).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V", [(3, 4000), (300, 4000), (1, 50001), (11, 126325), (70, 131075)])
+@pytest.mark.parametrize("high", [6.0, 12.0, 30.0])
+def test_a_likely_token_and_a_reference_that_prefers_another(n, V, dtype, high):
+    """The row's largest logit and the reference's lie far apart, in different parts of a row that is split."""
+    z, tok, d = make_policy(n, V, dtype, "logits", seed=9)
+    z.clamp_(max=8.0)
+    d["ref_logits"].clamp_(max=8.0)
+    g = torch.Generator().manual_seed(V)
+    at = torch.randint(0, V // 3, (n,), generator=g).cuda()
+    rows = torch.arange(n, device="cuda")
+    z[rows, at] = 10.0 + high
+    d["ref_logits"][rows, at + V // 2] = 12.0 + high
+    # few tokens are likely, and those are the ones that old_logp moves with
+    d["old_logp"] = (torch.log_softmax(z.double(), -1)[rows, tok.clamp(0, V - 1).long()] - 0.1).float()
+    kw = dict(clip_low=LO, clip_high=HI, c_kl=0.4, c_ent=0.02)
+    want = oracle(z, tok, **d, **kw)
+    check_policy(learn().policy_loss(z, tok, **d, **kw), want, dtype, V)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("V", [100, 40000])
 def test_numbers_that_are_not_finite_show(bad, V):
